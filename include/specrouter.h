@@ -72,7 +72,7 @@ enum {
   SR_ESCRATCH = -5,     /* the problem needs more workspace than the library's fixed array holds */
 };
 
-/* Logits element types. */
+/* Element types (logits, norm weights). */
 enum { SR_F32 = 0, SR_BF16 = 1 };
 
 /* Device-side data-error bits OR-ed into *status. */
@@ -84,6 +84,7 @@ enum {
   SR_ST_ROLLBACK_GROW = 16, /* rollback asked to grow a sequence (treated as a no-op) */
   SR_ST_TIMEOUT = 32,       /* not set since ABI version 4 (accept waits are bounded and recover) */
   SR_ST_CHAIN = 64,         /* accept lengths that one chain step cannot produce */
+  SR_ST_POSITION = 128,     /* a position outside the rotation table */
 };
 
 /* SPECROUTER_ABI_VERSION of the loaded library. */
@@ -351,6 +352,75 @@ int specrouter_kv_append(const void* k_new, const void* v_new, const int32_t* ga
                          int L_cap, int32_t* status, void* stream);
 int specrouter_kv_compact(void* k_cache, void* v_cache, uint8_t* cache_mask, int32_t* kv_len,
                           int B, int Hkv, int D, int L_cap, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Queries and keys of the new rows, before they are appended and attended to:
+ * every head x of D values, of row i <= gamma_b at position t = position[b] + i,
+ * becomes rot_t(norm(x)), with
+ *
+ *   norm(x) = x / sqrt(mean(x^2) + eps) * w      (x itself where w is NULL)
+ *   rot_t:  (y_a, y_c) -> (y_a cos - y_c sin, y_c cos + y_a sin)
+ *
+ * over rot_dim/2 pairs n, the angle's cosine and sine from
+ * rope_table[t][n] and rope_table[t][rot_dim/2 + n]: a = n, c = n + rot_dim/2,
+ * or with interleaved != 0 a = 2 n, c = 2 n + 1. Values from rot_dim on are not
+ * rotated. Any gamma_max >= 0: a step's gamma_b + 1 rows or whole prompts.
+ *
+ * q, k         bf16 [B][gamma_max+1][Hq or Hkv][D], D in {64, 128}; the heads of
+ *              a row are contiguous, and a row lies q_stride / k_stride ELEMENTS
+ *              (multiples of 8) after the one before it, so that both may be
+ *              views of one projection's output (16-byte aligned)
+ * q_weight, k_weight  [D] of weight_dtype (SR_F32 or SR_BF16), or NULL each
+ * rope_table   fp32 [max_positions][rot_dim] (16-byte aligned); rot_dim a
+ *              multiple of 16 up to D
+ * position     i32 [B]: of the sequence's row 0; position[b] must be in
+ *              [0, max_positions - gamma_b - 1], else SR_ST_POSITION
+ * gamma        i32 [B] in [0, gamma_max], else SR_ST_GAMMA
+ * q_out, k_out bf16 [B][gamma_max+1][Hq or Hkv][D] contiguous (what
+ *              specrouter_verify_attention and specrouter_kv_append take); may
+ *              be q / k themselves where those are contiguous, else they must
+ *              not overlap them
+ * Rows i > gamma_b, and all rows of a sequence with bad data, are neither read
+ * nor written. Computed in fp32 and rounded to bf16 once.
+ */
+int specrouter_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* q_weight,
+                            const void* k_weight, int weight_dtype, float eps, const float* rope_table,
+                            int max_positions, int rot_dim, int interleaved, const int32_t* position,
+                            const int32_t* gamma, void* q_out, void* k_out, int B, int gamma_max, int Hq, int Hkv,
+                            int D, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* A K/V cache held in 4 bits. For each of K and V:
+ *
+ * codes   u8 [B][Hkv][L_cap][D/2]   (16-byte aligned) two elements a byte, the
+ *         even one in the low half: bit 3 the sign, bits 0..2 one of
+ *         0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1)
+ * powers  u8 [B][Hkv][L_cap][D/32]  (4-byte aligned) p of each 32 consecutive
+ *         elements, which count 2^(p - 127) each; 255: all 32 are NaN
+ *
+ * 32 elements take 17 bytes, where bf16 takes 64.
+ *
+ * specrouter_kv4_append writes new rows as specrouter_kv_append does (same
+ * cursor, mask and lengths, same conditions that leave a sequence untouched),
+ * rounded: p is the least value from 1 to 252 with max |x| <= 7 * 2^(p - 127)
+ * over the 32 (252 if none is), each code the nearest (of two equally near the
+ * even code; above 6 it is 6), and 255 with codes 0 where one of the 32 is
+ * infinite or NaN. Any gamma_max < L_cap: a step's rows or whole prompts.
+ *
+ * k_new, v_new  bf16 [B][gamma_max+1][Hkv][D], rows k_stride / v_stride ELEMENTS
+ *               apart (multiples of 8; 16-byte aligned)
+ * k_seen, v_seen  bf16 [B][gamma_max+1][Hkv][D] out, or NULL each: the rows as
+ *               the cache now holds them, for attention among a prompt's own
+ *               rows. Rows i > gamma_b and those of an untouched sequence are
+ *               not written
+ * shared_len    i32 [1] or NULL, not an element of kv_len
+ * Everything else as for specrouter_kv_append; lengths, mask and rollback of
+ * such a cache are those of a bf16 one.
+ */
+int specrouter_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                          const int32_t* gamma, void* k_codes, void* k_powers, void* v_codes, void* v_powers,
+                          uint8_t* cache_mask, int32_t* kv_len, const int32_t* shared_len, void* k_seen, void* v_seen,
+                          int B, int gamma_max, int Hkv, int D, int L_cap, int32_t* status, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Multi-level chains (Section 3.1, multi-level verification; Section 4.3,

@@ -15,8 +15,10 @@ from ._lib import (
     SR_F32,
     AcceptBuffers,
     ChainScheduler,
+    Kv4Cache,
     attention_workspace,
     load,
+    rope_table,
     specrouter_abi_version,
     specrouter_accept_and_diverge,
     specrouter_accept_and_diverge_sampled,
@@ -26,8 +28,10 @@ from ._lib import (
     specrouter_chain_consensus,
     specrouter_chain_window,
     specrouter_hbm_read_probe,
+    specrouter_kv4_append,
     specrouter_kv_append,
     specrouter_kv_compact,
+    specrouter_qk_norm_rope,
     specrouter_rollback,
     specrouter_status_string,
     specrouter_verify_attention,
@@ -40,8 +44,10 @@ __all__ = [
     "SR_F32",
     "AcceptBuffers",
     "ChainScheduler",
+    "Kv4Cache",
     "attention_workspace",
     "load",
+    "rope_table",
     "specrouter_abi_version",
     "specrouter_accept_and_diverge",
     "specrouter_accept_and_diverge_sampled",
@@ -51,8 +57,10 @@ __all__ = [
     "specrouter_chain_consensus",
     "specrouter_chain_window",
     "specrouter_hbm_read_probe",
+    "specrouter_kv4_append",
     "specrouter_kv_append",
     "specrouter_kv_compact",
+    "specrouter_qk_norm_rope",
     "specrouter_rollback",
     "specrouter_status_string",
     "specrouter_verify_attention",

@@ -23,6 +23,7 @@ HEADERS = [os.path.join(INCLUDE, h) for h in ("specrouter.h", "specrouter_sched.
 SR_OK, SR_EINVAL, SR_EUNSUPPORTED, SR_EWORKSPACE, SR_ELAUNCH, SR_ESCRATCH = 0, -1, -2, -3, -4, -5
 SR_F32, SR_BF16 = 0, 1
 SR_ST_GAMMA, SR_ST_KVLEN, SR_ST_TOKEN, SR_ST_UNIFORM, SR_ST_ROLLBACK_GROW, SR_ST_TIMEOUT, SR_ST_CHAIN = 1, 2, 4, 8, 16, 32, 64
+SR_ST_POSITION = 128
 
 _c_p = ctypes.c_void_p
 _c_i = ctypes.c_int
@@ -71,6 +72,12 @@ _SIGNATURES = {
     "specrouter_chain_window": (_c_i, [_c_p, _c_p, _c_i, _c_i, _c_i] + [_c_p] * 5),
     "specrouter_kv_append": (_c_i, [_c_p] * 8 + [_c_i] * 5 + [_c_p, _c_p]),
     "specrouter_kv_compact": (_c_i, [_c_p] * 4 + [_c_i] * 4 + [_c_p, _c_p]),
+    "specrouter_qk_norm_rope": (
+        _c_i,
+        [_c_p, _c_i64, _c_p, _c_i64, _c_p, _c_p, _c_i, _c_f, _c_p, _c_i, _c_i, _c_i] + [_c_p] * 4 + [_c_i] * 5
+        + [_c_p, _c_p],
+    ),
+    "specrouter_kv4_append": (_c_i, [_c_p, _c_i64, _c_p, _c_i64] + [_c_p] * 10 + [_c_i] * 5 + [_c_p, _c_p]),
     "specrouter_chain_consensus": (_c_i, [_c_p, _c_p, _c_p, _c_i, _c_p, _c_p, _c_i, _c_i] + [_c_p] * 6),
     "specrouter_hbm_read_probe": (_c_i, [_c_p, _c_sz, _c_p, _c_p]),
     # chain scheduler (host code; host pointers)
@@ -135,6 +142,7 @@ def _check(rc: int, what: str) -> None:
 
 
 _INT32 = torch.int32
+_BF16 = torch.bfloat16
 
 
 def _dev(*ts):
@@ -418,8 +426,129 @@ def specrouter_kv_compact(k_cache, v_cache, cache_mask, kv_len, status=None):
     _check(rc, "specrouter_kv_compact")
 
 
+def _here(*ts):
+    """All tensors on the current device (whose stream the call goes to)."""
+    cur = torch._C._cuda_getDevice()
+    for t in ts:
+        if t is not None and t.get_device() != cur:
+            raise ValueError("all tensors must be on the current HIP device")
+
+
+def _shaped(t, shape, dtype, name):
+    """t is a contiguous tensor of this shape and type."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}")
+
+
+def _row_stride(t, name):
+    """Elements from one row of t [B, rows, H, D] to the next, one stride for the whole batch."""
+    B, rows, H, D = t.shape
+    s0, s1, s2, s3 = t.stride()
+    if t.dtype is not _BF16:
+        raise TypeError(f"{name} must be bfloat16")
+    row = s1 if rows > 1 else s0 if B > 1 else H * D
+    if (D > 1 and s3 != 1) or (H > 1 and s2 != D) or (B > 1 and rows > 1 and s0 != rows * s1):
+        raise ValueError(f"{name} must be [B, rows, H, D] with contiguous heads and evenly spaced rows")
+    return row
+
+
+def specrouter_qk_norm_rope(q, k, q_weight, k_weight, eps, rope_table, position, gamma, q_out, k_out,
+                            interleaved=False, status=None):
+    """q [B, rows, Hq, D] and k [B, rows, Hkv, D] bf16 (views of one projection
+    may be passed) -> q_out, k_out of the same shapes: every head normed (where
+    its weight [D] is not None) and rotated to its position. rope_table fp32
+    [max_positions, rot_dim] as from rope_table()."""
+    _here(q, k, q_weight, k_weight, rope_table, position, gamma, q_out, k_out, status)
+    B, rows, Hq, D = q.shape
+    Hkv = k.shape[2]
+    if k.shape != (B, rows, Hkv, D):
+        raise ValueError("q [B, rows, Hq, D] and k [B, rows, Hkv, D] expected")
+    _shaped(q_out, q.shape, _BF16, "q_out")
+    _shaped(k_out, k.shape, _BF16, "k_out")
+    _shaped(position, (B,), _INT32, "position")
+    _shaped(gamma, (B,), _INT32, "gamma")
+    code = SR_BF16
+    for w, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _shaped(w, (D,), w.dtype, n)
+            code = logits_dtype_code(w)
+    if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
+        raise TypeError("q_weight and k_weight must share a dtype")
+    if rope_table.dim() != 2:
+        raise ValueError("rope_table must be [max_positions, rot_dim]")
+    _shaped(rope_table, rope_table.shape, torch.float32, "rope_table")
+    rc = load().specrouter_qk_norm_rope(
+        q.data_ptr(), _row_stride(q, "q"), k.data_ptr(), _row_stride(k, "k"), _ptr(q_weight), _ptr(k_weight), code,
+        float(eps), rope_table.data_ptr(), rope_table.shape[0], rope_table.shape[1], 1 if interleaved else 0,
+        position.data_ptr(), gamma.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), B, rows - 1, Hq, Hkv, D,
+        _ptr(status), _stream())
+    _check(rc, "specrouter_qk_norm_rope")
+
+
+def _kv4_shapes(k_codes, k_powers, v_codes, v_powers, B, Hkv, D):
+    L_cap = k_codes.shape[2] if k_codes.dim() == 4 else -1
+    for t, w, n in ((k_codes, D // 2, "k_codes"), (k_powers, D // 32, "k_powers"), (v_codes, D // 2, "v_codes"),
+                    (v_powers, D // 32, "v_powers")):
+        _shaped(t, (B, Hkv, L_cap, w), torch.uint8, n)
+    return L_cap
+
+
+def _mask_of(cache_mask, B, L_cap):
+    if cache_mask is not None and (cache_mask.shape != (B, L_cap) or cache_mask.element_size() != 1
+                                   or not cache_mask.is_contiguous()):
+        raise ValueError("cache_mask must be u8 [B, L_cap]")
+
+
+def specrouter_kv4_append(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_powers, cache_mask, kv_len,
+                          shared_len=None, k_seen=None, v_seen=None, status=None):
+    """k_new/v_new [B, rows, Hkv, D] bf16 -> the 4-bit cache (codes
+    [B, Hkv, L_cap, D/2], powers [B, Hkv, L_cap, D/32], u8) at each cursor;
+    k_seen/v_seen [B, rows, Hkv, D] bf16: the rows as the cache now holds them."""
+    _here(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_powers, cache_mask, kv_len, shared_len, k_seen, v_seen,
+          status)
+    B, rows, Hkv, D = k_new.shape
+    if v_new.shape != k_new.shape:
+        raise ValueError("k_new and v_new must be [B, rows, Hkv, D]")
+    L_cap = _kv4_shapes(k_codes, k_powers, v_codes, v_powers, B, Hkv, D)
+    _mask_of(cache_mask, B, L_cap)
+    _shaped(gamma, (B,), _INT32, "gamma")
+    _shaped(kv_len, (B,), _INT32, "kv_len")
+    if shared_len is not None:
+        _shaped(shared_len, (1,), _INT32, "shared_len")
+    for t, n in ((k_seen, "k_seen"), (v_seen, "v_seen")):
+        if t is not None:
+            _shaped(t, k_new.shape, _BF16, n)
+    rc = load().specrouter_kv4_append(
+        k_new.data_ptr(), _row_stride(k_new, "k_new"), v_new.data_ptr(), _row_stride(v_new, "v_new"), gamma.data_ptr(),
+        k_codes.data_ptr(), k_powers.data_ptr(), v_codes.data_ptr(), v_powers.data_ptr(), _ptr(cache_mask),
+        kv_len.data_ptr(), _ptr(shared_len), _ptr(k_seen), _ptr(v_seen), B, rows - 1, Hkv, D, L_cap, _ptr(status),
+        _stream())
+    _check(rc, "specrouter_kv4_append")
+
+
 # ----------------------------------------------------------------------------
 # Buffer helpers (allocation only).
+
+def rope_table(max_positions, rot_dim, theta=10000.0, device="cuda"):
+    """fp32 [max_positions, rot_dim] for specrouter_qk_norm_rope: the cosines,
+    then the sines, of t * theta^(-2 n / rot_dim), n < rot_dim / 2, at every
+    position t (angles in 64 bits: at far positions 32 would lose them)."""
+    n = torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device)
+    t = torch.arange(max_positions, dtype=torch.float64, device=device)
+    angle = t[:, None] * theta ** (-n / rot_dim)
+    return torch.cat([angle.cos(), angle.sin()], -1).float()
+
+
+class Kv4Cache:
+    """An empty 4-bit K/V cache: k_codes, k_powers, v_codes, v_powers."""
+
+    def __init__(self, B: int, Hkv: int, L_cap: int, D: int, device="cuda"):
+        u8 = dict(dtype=torch.uint8, device=device)
+        self.k_codes = torch.zeros(B, Hkv, L_cap, D // 2, **u8)
+        self.k_powers = torch.zeros(B, Hkv, L_cap, D // 32, **u8)
+        self.v_codes = torch.zeros(B, Hkv, L_cap, D // 2, **u8)
+        self.v_powers = torch.zeros(B, Hkv, L_cap, D // 32, **u8)
+
 
 class AcceptBuffers:
     """Outputs and the self-resetting workspace of one accept-and-diverge call shape."""

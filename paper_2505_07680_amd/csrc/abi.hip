@@ -57,6 +57,12 @@ bool attention_shape_ok(int B, int gamma_max, int Hq, int Hkv, int L_cap) {
          Hq % Hkv == 0 && L_cap >= gamma_max + 1 && L_cap <= SPECROUTER_MAX_CACHE_ROWS && B <= 65535;
 }
 
+// Rows of a step or of a prompt: all of a batch's rows, with their heads, counted in 31 bits.
+bool rows_ok(int B, int gamma_max, int heads) {
+  return B > 0 && gamma_max >= 0 && heads > 0 && heads <= 65535 &&
+         ((int64_t)gamma_max + 1) * heads <= (int64_t)0x7fffffff / B;
+}
+
 // Checks and launch shared by the accept entry points (rollback NULL: none).
 int accept_impl(const void* p_logits, int64_t p_batch_stride, const void* q_logits, int64_t q_batch_stride,
                 int logits_dtype, const int32_t* draft_tokens, const int32_t* gamma, const float* u_accept,
@@ -114,6 +120,7 @@ const char* specrouter_status_string(int code) {
     case SR_ST_UNIFORM: return "device data: uniform outside [0, 1)";
     case SR_ST_ROLLBACK_GROW: return "device data: rollback would grow a sequence (ignored)";
     case SR_ST_TIMEOUT: return "device: inter-workgroup wait timed out";
+    case SR_ST_POSITION: return "device data: a position outside the rotation table";
     case SR_ST_CHAIN: return "device data: accept lengths one chain step cannot produce";
     default: return "unknown code";
   }
@@ -242,6 +249,47 @@ int specrouter_kv_compact(void* k_cache, void* v_cache, uint8_t* cache_mask, int
   if (!k_cache || !v_cache || !cache_mask || !kv_len) return SR_EINVAL;
   if (!aligned16(k_cache) || !aligned16(v_cache)) return SR_EINVAL;
   return sr::launch_kv_compact(k_cache, v_cache, cache_mask, kv_len, B, Hkv, D, L_cap, status, (hipStream_t)stream);
+}
+
+int specrouter_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* q_weight,
+                            const void* k_weight, int weight_dtype, float eps, const float* rope_table,
+                            int max_positions, int rot_dim, int interleaved, const int32_t* position,
+                            const int32_t* gamma, void* q_out, void* k_out, int B, int gamma_max, int Hq, int Hkv,
+                            int D, int32_t* status, void* stream) {
+  if (!q || !k || !rope_table || !position || !gamma || !q_out || !k_out) return SR_EINVAL;
+  if (Hq <= 0 || Hkv <= 0 || Hq > 65535 || Hkv > 65535 || !rows_ok(B, gamma_max, Hq + Hkv)) return SR_EINVAL;
+  if (D != 64 && D != 128) return SR_EUNSUPPORTED;
+  if (weight_dtype != SR_F32 && weight_dtype != SR_BF16) return SR_EUNSUPPORTED;
+  if (max_positions <= 0 || rot_dim <= 0 || rot_dim > D || rot_dim % 16 != 0) return SR_EINVAL;
+  if (!(eps >= 0.f && eps < __builtin_inff())) return SR_EINVAL;
+  if (q_stride < (int64_t)Hq * D || k_stride < (int64_t)Hkv * D || q_stride % 8 != 0 || k_stride % 8 != 0)
+    return SR_EINVAL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(rope_table) ||
+      !aligned16(q_weight) || !aligned16(k_weight))
+    return SR_EINVAL;
+  // in place only where input and output rows are the same rows
+  if ((q_out == q && q_stride != (int64_t)Hq * D) || (k_out == k && k_stride != (int64_t)Hkv * D)) return SR_EINVAL;
+  return sr::launch_qk_norm_rope(q, q_stride, k, k_stride, q_weight, k_weight, weight_dtype == SR_F32, eps, rope_table,
+                                 max_positions, rot_dim, interleaved != 0, position, gamma, q_out, k_out, B, gamma_max,
+                                 Hq, Hkv, D, status, (hipStream_t)stream);
+}
+
+int specrouter_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                          const int32_t* gamma, void* k_codes, void* k_powers, void* v_codes, void* v_powers,
+                          uint8_t* cache_mask, int32_t* kv_len, const int32_t* shared_len, void* k_seen, void* v_seen,
+                          int B, int gamma_max, int Hkv, int D, int L_cap, int32_t* status, void* stream) {
+  if (!k_new || !v_new || !gamma || !k_codes || !k_powers || !v_codes || !v_powers || !kv_len) return SR_EINVAL;
+  if (B > 65535 || Hkv <= 0 || Hkv > 65535 || !rows_ok(B, gamma_max, Hkv)) return SR_EINVAL;
+  if (L_cap < 1 || L_cap > SPECROUTER_MAX_CACHE_ROWS || gamma_max >= L_cap) return SR_EINVAL;
+  if (D != 64 && D != 128) return SR_EUNSUPPORTED;
+  if (k_stride < (int64_t)Hkv * D || v_stride < (int64_t)Hkv * D || k_stride % 8 != 0 || v_stride % 8 != 0)
+    return SR_EINVAL;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_codes) || !aligned16(v_codes) || !aligned16(k_seen) ||
+      !aligned16(v_seen) || ((uintptr_t)k_powers & 3u) != 0 || ((uintptr_t)v_powers & 3u) != 0)
+    return SR_EINVAL;
+  return sr::launch_kv4_append(k_new, k_stride, v_new, v_stride, gamma, k_codes, k_powers, v_codes, v_powers,
+                               cache_mask, kv_len, shared_len, k_seen, v_seen, B, gamma_max, Hkv, D, L_cap, status,
+                               (hipStream_t)stream);
 }
 
 int specrouter_rollback(int32_t* kv_len, uint8_t* cache_mask, const int32_t* new_len,

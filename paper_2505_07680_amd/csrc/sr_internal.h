@@ -323,6 +323,15 @@ int launch_kv_append(const void* k_new, const void* v_new, const int32_t* gamma,
 int launch_kv_compact(void* k_cache, void* v_cache, uint8_t* cache_mask, int32_t* kv_len, int B, int Hkv, int D,
                       int L_cap, int32_t* status, hipStream_t stream);
 
+int launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* q_weight,
+                        const void* k_weight, bool w_f32, float eps, const float* table, int max_positions, int rot,
+                        bool adjacent, const int32_t* position, const int32_t* gamma, void* q_out, void* k_out, int B,
+                        int gamma_max, int Hq, int Hkv, int D, int32_t* status, hipStream_t stream);
+int launch_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* gamma,
+                      void* k_codes, void* k_powers, void* v_codes, void* v_powers, uint8_t* cache_mask,
+                      int32_t* kv_len, const int32_t* shared_len, void* k_seen, void* v_seen, int B, int gamma_max,
+                      int Hkv, int D, int L_cap, int32_t* status, hipStream_t stream);
+
 int launch_rollback(int32_t* kv_len, uint8_t* cache_mask, const int32_t* new_len,
                     int32_t* phys_len, int B, int L_cap, int32_t* status, hipStream_t stream);
 

@@ -1,0 +1,70 @@
+"""Host-side argument checks of the calls around the attention, on the CPU: every
+bad argument is refused before anything touches the device."""
+
+import ctypes
+import os
+
+import pytest
+
+from paper_2505_07680_amd import _lib
+
+no_device = pytest.mark.skipif(
+    __import__("torch").cuda.device_count() > 0, reason="host-only argument checks"
+)
+EINVAL, EUNSUPPORTED, EWORKSPACE, ELAUNCH = _lib.SR_EINVAL, _lib.SR_EUNSUPPORTED, _lib.SR_EWORKSPACE, _lib.SR_ELAUNCH
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(_lib.LIB_PATH):
+        from paper_2505_07680_amd.build import build
+
+        build()
+    return _lib.load()
+
+
+P = ctypes.c_void_p(4096)  # never dereferenced: every case ends before a launch
+ODD = ctypes.c_void_p(4104)
+
+
+def _refusals(call, good, cases):
+    assert call(*good) == ELAUNCH  # fine but for the device, of which there is none here
+    for at, value, want in cases:
+        args = list(good)
+        args[at] = value
+        assert call(*args) == want, (at, value)
+
+
+def test_position_bit_has_a_text(lib):
+    assert b"position" in lib.specrouter_status_string(_lib.SR_ST_POSITION)
+
+
+@no_device
+def test_norm_rope(lib):
+    # q, stride, k, stride, wq, wk, dtype, eps, table, max_pos, rot, pairs, pos, gamma, qo, ko, B, gmax, Hq, Hkv, D, status, stream
+    good = [P, 512, P, 128, None, None, 0, 1e-6, P, 100, 64, 0, P, P, ctypes.c_void_p(8192), ctypes.c_void_p(16384),
+            2, 3, 8, 2, 64, None, None]
+    cases = [(i, None, EINVAL) for i in (0, 2, 8, 12, 13, 14, 15)]
+    cases += [(i, ODD, EINVAL) for i in (0, 2, 4, 5, 8, 14, 15)]
+    cases += [(1, 504, EINVAL), (1, 516, EINVAL), (3, 120, EINVAL), (6, 2, EUNSUPPORTED), (7, -1e-6, EINVAL),
+              (7, float("nan"), EINVAL), (7, float("inf"), EINVAL), (9, 0, EINVAL), (10, 0, EINVAL), (10, 24, EINVAL),
+              (10, 80, EINVAL), (16, 0, EINVAL), (17, -1, EINVAL), (18, 0, EINVAL), (19, 0, EINVAL),
+              (18, 1 << 20, EINVAL), (20, 96, EUNSUPPORTED), (17, 2 ** 31 - 1, EINVAL), (16, 2 ** 31 - 1, EINVAL)]
+    _refusals(lib.specrouter_qk_norm_rope, good, cases)
+    apart = list(good)
+    apart[1], apart[14] = 1024, P  # in place, with the rows of a wider projection
+    assert lib.specrouter_qk_norm_rope(*apart) == EINVAL
+    apart[1] = 512
+    assert lib.specrouter_qk_norm_rope(*apart) == ELAUNCH
+
+
+@no_device
+def test_kv4_append(lib):
+    # k, stride, v, stride, gamma, kc, kp, vc, vp, mask, kv_len, shared, k_seen, v_seen, B, gmax, Hkv, D, L_cap, status, stream
+    good = [P, 128, P, 128, P, P, P, P, P, None, P, None, None, None, 2, 3, 2, 64, 100, None, None]
+    cases = [(i, None, EINVAL) for i in (0, 2, 4, 5, 6, 7, 8, 10)]
+    cases += [(i, ODD, EINVAL) for i in (0, 2, 5, 7, 12, 13)]
+    cases += [(i, ctypes.c_void_p(4098), EINVAL) for i in (6, 8)]
+    cases += [(1, 120, EINVAL), (3, 132, EINVAL), (14, 0, EINVAL), (14, 65536, EINVAL), (15, -1, EINVAL),
+              (15, 100, EINVAL), (16, 0, EINVAL), (17, 32, EUNSUPPORTED), (18, 0, EINVAL), (18, (1 << 22) + 1, EINVAL)]
+    _refusals(lib.specrouter_kv4_append, good, cases)
