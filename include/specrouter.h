@@ -135,6 +135,30 @@ int specrouter_verify_attention(const void* q, const void* k_cache, const void* 
                                 size_t workspace_bytes, int32_t* status, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Verification attention with a sliding window and sinks: as
+ * specrouter_verify_attention, but the row at cache position pos sees, of the
+ * keys j <= pos with cache_mask[b][j] != 0, those with j > pos - window or
+ * j < sinks. Positions are cache rows, masked ones counted. Only the rows that
+ * some new row can see are read: at most window + gamma_b + sinks per sequence
+ * and kv head, and what lies between the sinks and the window is ignored
+ * whatever it holds.
+ *
+ * window     >= 1 (from L_cap on it hides nothing); sinks >= 0; else SR_EINVAL
+ * out        [B][gamma_max+1][Hq][D] of out_dtype: SR_F32, or SR_BF16 (the same
+ *            values rounded once)
+ * workspace  of specrouter_verify_attention_window_workspace_size() bytes for the
+ *            same arguments, zero-filled before its first use (as above)
+ * All other arguments, errors and the precision as for specrouter_verify_attention.
+ */
+size_t specrouter_verify_attention_window_workspace_size(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap,
+                                                         int window, int sinks);
+int specrouter_verify_attention_window(const void* q, const void* k_cache, const void* v_cache,
+                                       const uint8_t* cache_mask, const int32_t* kv_len, const int32_t* gamma,
+                                       void* out, int out_dtype, int B, int gamma_max, int Hq, int Hkv, int D,
+                                       int L_cap, int window, int sinks, float scale, void* workspace,
+                                       size_t workspace_bytes, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Accept and diverge (Section 2.2 steps 3-4, probabilistic acceptance; Eq. 2;
  * Eq. 5), one sweep over the logits.
  *
@@ -421,6 +445,21 @@ int specrouter_kv4_append(const void* k_new, int64_t k_stride, const void* v_new
                           const int32_t* gamma, void* k_codes, void* k_powers, void* v_codes, void* v_powers,
                           uint8_t* cache_mask, int32_t* kv_len, const int32_t* shared_len, void* k_seen, void* v_seen,
                           int B, int gamma_max, int Hkv, int D, int L_cap, int32_t* status, void* stream);
+
+/* Verification attention over such a cache: specrouter_verify_attention (window
+ * 0) or specrouter_verify_attention_window (window >= 1) with K and V the values
+ * that codes and powers stand for, which the products take exactly. Entries that
+ * no new row sees are ignored whatever they hold. out_dtype as for the window
+ * call; workspace of specrouter_verify_attention_kv4_workspace_size() bytes for
+ * the same arguments, zero-filled before its first use.
+ */
+size_t specrouter_verify_attention_kv4_workspace_size(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap,
+                                                      int window, int sinks);
+int specrouter_verify_attention_kv4(const void* q, const void* k_codes, const void* k_powers, const void* v_codes,
+                                    const void* v_powers, const uint8_t* cache_mask, const int32_t* kv_len,
+                                    const int32_t* gamma, void* out, int out_dtype, int B, int gamma_max, int Hq,
+                                    int Hkv, int D, int L_cap, int window, int sinks, float scale, void* workspace,
+                                    size_t workspace_bytes, int32_t* status, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Multi-level chains (Section 3.1, multi-level verification; Section 4.3,

@@ -16,6 +16,8 @@ from ._lib import (
     AcceptBuffers,
     ChainScheduler,
     Kv4Cache,
+    attention_kv4_workspace,
+    attention_window_workspace,
     attention_workspace,
     load,
     rope_table,
@@ -35,6 +37,10 @@ from ._lib import (
     specrouter_rollback,
     specrouter_status_string,
     specrouter_verify_attention,
+    specrouter_verify_attention_kv4,
+    specrouter_verify_attention_kv4_workspace_size,
+    specrouter_verify_attention_window,
+    specrouter_verify_attention_window_workspace_size,
     specrouter_verify_attention_workspace_size,
 )
 
@@ -45,6 +51,8 @@ __all__ = [
     "AcceptBuffers",
     "ChainScheduler",
     "Kv4Cache",
+    "attention_kv4_workspace",
+    "attention_window_workspace",
     "attention_workspace",
     "load",
     "rope_table",
@@ -64,5 +72,9 @@ __all__ = [
     "specrouter_rollback",
     "specrouter_status_string",
     "specrouter_verify_attention",
+    "specrouter_verify_attention_kv4",
+    "specrouter_verify_attention_kv4_workspace_size",
+    "specrouter_verify_attention_window",
+    "specrouter_verify_attention_window_workspace_size",
     "specrouter_verify_attention_workspace_size",
 ]

@@ -48,6 +48,16 @@ _SIGNATURES = {
         _c_i,
         [_c_p] * 7 + [_c_i] * 6 + [_c_f, _c_p, _c_sz, _c_p, _c_p],
     ),
+    "specrouter_verify_attention_window_workspace_size": (_c_sz, [_c_i] * 8),
+    "specrouter_verify_attention_window": (
+        _c_i,
+        [_c_p] * 7 + [_c_i] * 9 + [_c_f, _c_p, _c_sz, _c_p, _c_p],
+    ),
+    "specrouter_verify_attention_kv4_workspace_size": (_c_sz, [_c_i] * 8),
+    "specrouter_verify_attention_kv4": (
+        _c_i,
+        [_c_p] * 9 + [_c_i] * 9 + [_c_f, _c_p, _c_sz, _c_p, _c_p],
+    ),
     "specrouter_accept_workspace_size": (_c_sz, [_c_i] * 4),
     "specrouter_accept_and_diverge": (
         _c_i,
@@ -526,6 +536,70 @@ def specrouter_kv4_append(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_pow
     _check(rc, "specrouter_kv4_append")
 
 
+def specrouter_verify_attention_window_workspace_size(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks) -> int:
+    return load().specrouter_verify_attention_window_workspace_size(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks)
+
+
+def specrouter_verify_attention_kv4_workspace_size(B, gamma_max, Hq, Hkv, D, L_cap, window=0, sinks=0) -> int:
+    return load().specrouter_verify_attention_kv4_workspace_size(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks)
+
+
+def _out_code(out, shape):
+    if out.shape != shape or not out.is_contiguous():
+        raise ValueError("out must be contiguous [B, gamma_max+1, Hq, D]")
+    if out.dtype is _BF16:
+        return SR_BF16
+    if out.dtype is torch.float32:
+        return SR_F32
+    raise TypeError("out must be float32 or bfloat16")
+
+
+def specrouter_verify_attention_window(q, k_cache, v_cache, cache_mask, kv_len, gamma, out, scale, window, sinks=0,
+                                       workspace=None, status=None):
+    """specrouter_verify_attention where a row sees the last `window` cache rows
+    up to its own and the first `sinks`; out [B, gmax+1, Hq, D] fp32 or bf16."""
+    _here(q, k_cache, v_cache, cache_mask, kv_len, gamma, out, workspace, status)
+    B, G1, Hq, D = q.shape
+    Hkv, L_cap = k_cache.shape[1], k_cache.shape[2]
+    _shaped(q, q.shape, _BF16, "q")
+    _shaped(k_cache, (B, Hkv, L_cap, D), _BF16, "k_cache")
+    _shaped(v_cache, (B, Hkv, L_cap, D), _BF16, "v_cache")
+    _shaped(kv_len, (B,), _INT32, "kv_len")
+    _shaped(gamma, (B,), _INT32, "gamma")
+    _mask_of(cache_mask, B, L_cap)
+    code = _out_code(out, q.shape)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = load().specrouter_verify_attention_window(
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(cache_mask), kv_len.data_ptr(), gamma.data_ptr(),
+        out.data_ptr(), code, B, G1 - 1, Hq, Hkv, D, L_cap, int(window), int(sinks), float(scale), _ptr(workspace),
+        ws_bytes, _ptr(status), _stream())
+    _check(rc, "specrouter_verify_attention_window")
+    return out
+
+
+def specrouter_verify_attention_kv4(q, k_codes, k_powers, v_codes, v_powers, cache_mask, kv_len, gamma, out, scale,
+                                    window=0, sinks=0, workspace=None, status=None):
+    """The attention over a 4-bit cache (codes [B, Hkv, L_cap, D/2], powers
+    [B, Hkv, L_cap, D/32], u8), of all keys (window 0) or a window and sinks;
+    out [B, gmax+1, Hq, D] fp32 or bf16."""
+    _here(q, k_codes, k_powers, v_codes, v_powers, cache_mask, kv_len, gamma, out, workspace, status)
+    B, G1, Hq, D = q.shape
+    Hkv = k_codes.shape[1]
+    _shaped(q, q.shape, _BF16, "q")
+    L_cap = _kv4_shapes(k_codes, k_powers, v_codes, v_powers, B, Hkv, D)
+    _shaped(kv_len, (B,), _INT32, "kv_len")
+    _shaped(gamma, (B,), _INT32, "gamma")
+    _mask_of(cache_mask, B, L_cap)
+    code = _out_code(out, q.shape)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = load().specrouter_verify_attention_kv4(
+        q.data_ptr(), k_codes.data_ptr(), k_powers.data_ptr(), v_codes.data_ptr(), v_powers.data_ptr(),
+        _ptr(cache_mask), kv_len.data_ptr(), gamma.data_ptr(), out.data_ptr(), code, B, G1 - 1, Hq, Hkv, D, L_cap,
+        int(window), int(sinks), float(scale), _ptr(workspace), ws_bytes, _ptr(status), _stream())
+    _check(rc, "specrouter_verify_attention_kv4")
+    return out
+
+
 # ----------------------------------------------------------------------------
 # Buffer helpers (allocation only).
 
@@ -573,6 +647,16 @@ class AcceptBuffers:
 
 def attention_workspace(B, gamma_max, Hq, Hkv, D, L_cap, device="cuda"):
     n = specrouter_verify_attention_workspace_size(B, gamma_max, Hq, Hkv, D, L_cap)
+    return None if n == 0 else torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def attention_window_workspace(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks=0, device="cuda"):
+    n = specrouter_verify_attention_window_workspace_size(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks)
+    return None if n == 0 else torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def attention_kv4_workspace(B, gamma_max, Hq, Hkv, D, L_cap, window=0, sinks=0, device="cuda"):
+    n = specrouter_verify_attention_kv4_workspace_size(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks)
     return None if n == 0 else torch.zeros(n, dtype=torch.uint8, device=device)
 
 

@@ -50,6 +50,9 @@ int resident_per_cu(const void* fn, int threads, size_t lds) {
 
 namespace {
 
+// Workgroups of a launch: up to 512 threads each, 2^32 of them in all.
+constexpr int64_t kMaxGroups = ((int64_t)1 << 32) / 512 - 1;
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 bool attention_shape_ok(int B, int gamma_max, int Hq, int Hkv, int L_cap) {
@@ -130,7 +133,7 @@ size_t specrouter_verify_attention_workspace_size(int B, int gamma_max, int Hq, 
                                                   int L_cap) {
   if (!attention_shape_ok(B, gamma_max, Hq, Hkv, L_cap) || (D != 64 && D != 128)) return 0;
   sr::AttentionPlan plan;
-  if (sr::attention_plan(B, gamma_max, Hq, Hkv, D, L_cap, &plan) != SR_OK) return 0;
+  if (sr::attention_plan(B, gamma_max, Hq, Hkv, D, L_cap, 0, 0, &plan) != SR_OK) return 0;
   return plan.workspace_bytes;
 }
 
@@ -145,14 +148,76 @@ int specrouter_verify_attention(const void* q, const void* k_cache, const void* 
   if (!(scale > 0.f && scale < __builtin_inff())) return SR_EINVAL;  // a positive, finite score scale
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return SR_EINVAL;
   sr::AttentionPlan plan;
-  const int rc = sr::attention_plan(B, gamma_max, Hq, Hkv, D, L_cap, &plan);
+  const int rc = sr::attention_plan(B, gamma_max, Hq, Hkv, D, L_cap, 0, 0, &plan);
   if (rc != SR_OK) return rc;
   if (plan.workspace_bytes > 0 &&
       (!workspace || workspace_bytes < plan.workspace_bytes || !aligned16(workspace)))
     return SR_EWORKSPACE;
-  return sr::launch_verify_attention(q, k_cache, v_cache, cache_mask, kv_len, gamma, out, B,
-                                     gamma_max, Hq, Hkv, D, L_cap, scale, workspace, plan, status,
+  return sr::launch_verify_attention(q, k_cache, v_cache, cache_mask, kv_len, gamma, out, false, B,
+                                     gamma_max, Hq, Hkv, D, L_cap, 0, 0, scale, workspace, plan, status,
                                      (hipStream_t)stream);
+}
+
+size_t specrouter_verify_attention_window_workspace_size(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap,
+                                                         int window, int sinks) {
+  if (!attention_shape_ok(B, gamma_max, Hq, Hkv, L_cap) || (D != 64 && D != 128) || window < 1 || sinks < 0) return 0;
+  sr::AttentionPlan plan;
+  if (sr::attention_plan(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks, &plan) != SR_OK) return 0;
+  return plan.workspace_bytes;
+}
+
+int specrouter_verify_attention_window(const void* q, const void* k_cache, const void* v_cache,
+                                       const uint8_t* cache_mask, const int32_t* kv_len, const int32_t* gamma,
+                                       void* out, int out_dtype, int B, int gamma_max, int Hq, int Hkv, int D,
+                                       int L_cap, int window, int sinks, float scale, void* workspace,
+                                       size_t workspace_bytes, int32_t* status, void* stream) {
+  if (!q || !k_cache || !v_cache || !kv_len || !gamma || !out) return SR_EINVAL;
+  if (!attention_shape_ok(B, gamma_max, Hq, Hkv, L_cap) || window < 1 || sinks < 0) return SR_EINVAL;
+  if (D != 64 && D != 128) return SR_EUNSUPPORTED;
+  if (out_dtype != SR_F32 && out_dtype != SR_BF16) return SR_EUNSUPPORTED;
+  if (!(scale > 0.f && scale < __builtin_inff())) return SR_EINVAL;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return SR_EINVAL;
+  sr::AttentionPlan plan;
+  const int rc = sr::attention_plan(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks, &plan);
+  if (rc != SR_OK) return rc;
+  if ((int64_t)plan.n_splits * plan.q_chunks * B * Hkv > kMaxGroups) return SR_EINVAL;
+  if (plan.workspace_bytes > 0 && (!workspace || workspace_bytes < plan.workspace_bytes || !aligned16(workspace)))
+    return SR_EWORKSPACE;
+  return sr::launch_verify_attention(q, k_cache, v_cache, cache_mask, kv_len, gamma, out, out_dtype == SR_BF16, B,
+                                     gamma_max, Hq, Hkv, D, L_cap, window, sinks, scale, workspace, plan, status,
+                                     (hipStream_t)stream);
+}
+
+size_t specrouter_verify_attention_kv4_workspace_size(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap,
+                                                      int window, int sinks) {
+  if (!attention_shape_ok(B, gamma_max, Hq, Hkv, L_cap) || (D != 64 && D != 128) || window < 0 || sinks < 0) return 0;
+  sr::AttentionPlan plan;
+  if (sr::attention_kv4_plan(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks, &plan) != SR_OK) return 0;
+  return plan.workspace_bytes;
+}
+
+int specrouter_verify_attention_kv4(const void* q, const void* k_codes, const void* k_powers, const void* v_codes,
+                                    const void* v_powers, const uint8_t* cache_mask, const int32_t* kv_len,
+                                    const int32_t* gamma, void* out, int out_dtype, int B, int gamma_max, int Hq,
+                                    int Hkv, int D, int L_cap, int window, int sinks, float scale, void* workspace,
+                                    size_t workspace_bytes, int32_t* status, void* stream) {
+  if (!q || !k_codes || !k_powers || !v_codes || !v_powers || !kv_len || !gamma || !out) return SR_EINVAL;
+  if (!attention_shape_ok(B, gamma_max, Hq, Hkv, L_cap) || window < 0 || sinks < 0) return SR_EINVAL;
+  if (D != 64 && D != 128) return SR_EUNSUPPORTED;
+  if (out_dtype != SR_F32 && out_dtype != SR_BF16) return SR_EUNSUPPORTED;
+  if (!(scale > 0.f && scale < __builtin_inff())) return SR_EINVAL;
+  if (!aligned16(q) || !aligned16(k_codes) || !aligned16(v_codes) || !aligned16(out) ||
+      ((uintptr_t)k_powers & 3u) != 0 || ((uintptr_t)v_powers & 3u) != 0)
+    return SR_EINVAL;
+  sr::AttentionPlan plan;
+  const int rc = sr::attention_kv4_plan(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks, &plan);
+  if (rc != SR_OK) return rc;
+  if ((int64_t)plan.n_splits * plan.q_chunks * B * Hkv > kMaxGroups) return SR_EINVAL;
+  if (plan.workspace_bytes > 0 && (!workspace || workspace_bytes < plan.workspace_bytes || !aligned16(workspace)))
+    return SR_EWORKSPACE;
+  return sr::launch_attention_kv4(q, k_codes, k_powers, v_codes, v_powers, cache_mask, kv_len, gamma, out,
+                                  out_dtype == SR_BF16, B, gamma_max, Hq, Hkv, D, L_cap, window, sinks, scale,
+                                  workspace, plan, status, (hipStream_t)stream);
 }
 
 size_t specrouter_accept_workspace_size(int B, int gamma_max, int V, int logits_dtype) {

@@ -43,38 +43,28 @@
 //     V^T operand comes from the LDS transposing read.
 // Scores are kept in log2 units (scale * log2(e) folded in) and exponentiated
 // with exp2.
+//
+// With a window (WIN) a row at position pos sees the keys above pos - window and
+// the cache's first `sinks`. Only the tiles that hold such keys are taken: they
+// are numbered without the gap between the sinks and row 0's first key, and
+// splits and streams deal those numbers as they deal all tiles otherwise. V rows
+// that no row sees are zeroed like masked ones. The kernel without a window is
+// compiled apart, so that it pays nothing for this.
 
-#include "sr_internal.h"
+#include "attention_common.h"
 
 namespace sr {
 namespace {
 
-typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef float floatx2 __attribute__((ext_vector_type(2)));
-
-constexpr int kWaves = 4;  // key streams
 constexpr int kWaveKeys = 16;
 // At most three 16-row query blocks per wave (the accumulators stay in 256
 // registers at two waves per SIMD) and two query groups per workgroup: more
 // than 96 rows go to further query chunks, which read the same K/V again.
 constexpr int kMaxNQ = 3;
 constexpr int kMaxQG = 2;
-// How far (log2) a tile's maximum exceeds a row's softmax reference before that
-// is raised, and the same where it follows the tiles.
-constexpr float kLazy = 8.f;
+// The same where the reference follows the tiles.
 constexpr float kLazyFollow = 7.f;
-// Arrival counters sit one per 128-byte line: the splits of different
-// (sequence, kv head, query chunk) jobs then never contend for one line.
-constexpr int kCounterStride = 32;
 constexpr int kMaxSplitKeys = 8448;  // keys per split at most (about 4 MB of K/V at D = 128)
-// Byte offset past the end of any K/V slab (slabs are below 2^31 bytes): a
-// buffer load there returns zero without touching memory.
-constexpr uint32_t kOutOfRange = 0x7ffffff0u;
-// Cache-policy operand of the K/V loads when one workgroup is the only
-// reader of its K/V tiles (a single query chunk): non-temporal. With several
-// query chunks the others re-read the same tiles, which then should stay in
-// the caches (plain loads).
-constexpr int kStreamLoad = 2;
 
 template <int D>
 struct Geo {
@@ -89,53 +79,13 @@ struct Geo {
   static constexpr int kWaveBytes = kSlotK + kWaveKeys * kVStride;
 };
 
-// Threads, ring depth and LDS buffers per slot of a workgroup with QG query
-// groups: with two groups each wave fetches half of a tile, so a four-deep
-// ring of half tiles holds the registers of a two-deep ring of whole ones.
-template <int QG>
-struct Shape {
-  static constexpr int kThreads = 64 * kWaves * QG;
-  static constexpr int kRing = QG == 1 ? 2 : 4;
-  static constexpr int kBufs = QG == 1 ? 1 : 2;
-};
-
 template <int D, int NQ, int QG>
 struct Lds {
   static constexpr int MQ = 16 * NQ;
   static constexpr int kStage = kWaves * Shape<QG>::kBufs * Geo<D>::kWaveBytes + QG * MQ * Geo<D>::kKStride;
-  // Merge of the four stream states of each query group: the columns are
-  // reduced in kPasses passes so that a group's four fp32 slices fit in 72 KB
-  // (two four-wave workgroups per CU, or one of eight, fit in its 160 KB).
-  static constexpr int kPasses = (kWaves * MQ * D * 4 <= 73728) ? 1 : (kWaves * MQ * D * 2 <= 73728) ? 2 : 4;
-  static constexpr int kDp = D / kPasses;                 // columns per pass
-  static constexpr int kRowStride = kDp + 4;              // floats; padded against bank conflicts
-  static constexpr int kSlot = MQ * kRowStride;           // floats per wave slice
-  static constexpr int kMl = QG * kWaves * kSlot * 4;     // byte offset of the (m, l) exchange
-  static constexpr int kComb = kMl + QG * (kWaves + 1) * 2 * MQ * 4;
+  static constexpr int kComb = MergeLds<D, NQ, QG>::kComb;
   static constexpr int kBytes = kStage > kComb ? kStage : kComb;
 };
-
-// 16-byte device-coherent (sc1) buffer access to the split partials; the
-// descriptor's range check turns an out-of-range offset into a dropped store
-// or a zero load.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t partial_rsrc(const float* base, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, (int)bytes, 0x00020000);
-}
-constexpr int kDeviceCoherent = 16;  // cache-policy operand: sc1
-
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-  const __bf16 a = (__bf16)lo;
-  const __bf16 b = (__bf16)hi;
-  return (uint32_t)__builtin_bit_cast(uint16_t, a) | ((uint32_t)__builtin_bit_cast(uint16_t, b) << 16);
-}
-
-// Order LDS accesses of one wave around a point (compiler barrier; the LDS
-// unit serves one wave's requests in order).
-__device__ __forceinline__ void wave_lds_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 
 template <int D, int QG>
 struct Stage {  // one wave's part of a 16-key tile in flight
@@ -164,15 +114,15 @@ __device__ __forceinline__ float next_ref(float mt, float m_run, bool grow) {
 // (168 registers), else two (256). Two groups of three blocks at D = 128 use all
 // 256 and keep three or four values in scratch that the ring's loop reads back
 // (six loads per round of four tiles).
-template <int D, int NQ, int QG, bool NT, bool FOLLOW>
+template <int D, int NQ, int QG, bool NT, bool FOLLOW, bool WIN>
 __global__ void __launch_bounds__(Shape<QG>::kThreads, NQ == 1 && QG == 1 ? 3 : 2)
 attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ kc,
                   const uint16_t* __restrict__ vc, const uint8_t* __restrict__ mask,
                   const int32_t* __restrict__ kv_len, const int32_t* __restrict__ gamma,
-                  float* __restrict__ out, float* __restrict__ part_o,
+                  void* __restrict__ out, bool out_bf16, float* __restrict__ part_o,
                   float* __restrict__ part_ml, uint32_t* __restrict__ counters,
                   const int32_t* __restrict__ order, int B, int gmax, int Hq, int Hkv, int L_cap,
-                  float scale_log2, int split_keys, int n_splits, int q_chunks,
+                  int window, int sinks, float scale_log2, int split_keys, int n_splits, int q_chunks,
                   int32_t* __restrict__ status) {
   using GG = Geo<D>;
   constexpr int MQ = 16 * NQ;
@@ -212,7 +162,9 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
   const int row0 = qc * QG * MQ;
   const int row_end = min(R, row0 + QG * MQ);
   const int Mb = valid ? G * (gam + 1) : 0;
-  const int ns = valid ? (L + split_keys - 1) / split_keys : 0;  // splits that hold keys
+  const Reach<kWaveKeys> reach(WIN && valid ? L - gam - 1 : 0, WIN && valid ? L : 0, WIN ? window : 1, WIN ? sinks : 0);
+  const int n_keys = !valid ? 0 : WIN ? reach.tiles * kWaveKeys : L;
+  const int ns = (n_keys + split_keys - 1) / split_keys;  // splits that hold keys
   const bool work = row0 < Mb && split < ns;
 
   const int tid = threadIdx.x;
@@ -224,6 +176,14 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
   const int l16 = lane & 15;
   const int lg = lane >> 4;
 
+  // Four columns of output row r. Without a window the output is fp32; with one,
+  // fp32 or bf16 (rounded once, from the 32-bit sums).
+  auto store = [&](int r, int col, const floatx4& x) __attribute__((always_inline)) {
+    const int i = r / G, hh = g * G + r % G;
+    const size_t at = ((size_t)(b * (gmax + 1) + i) * Hq + hh) * D + col;
+    if (WIN && out_bf16) *(u32x2*)((uint16_t*)out + at) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    else *(floatx4*)((float*)out + at) = x;
+  };
   if (!work) {
     // Nothing to compute. Split 0 of a query chunk without live rows (or of an
     // invalid sequence) owns those output rows and writes them as zero.
@@ -231,8 +191,7 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
       for (int idx = tid; idx < (row_end - row0) * (D / 4); idx += kT) {
         const int r = row0 + idx / (D / 4);
         const int d4 = idx % (D / 4);
-        const int i = r / G, hh = g * G + r % G;
-        *(float4*)(out + ((size_t)(b * (gmax + 1) + i) * Hq + hh) * D + d4 * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+        store(r, d4 * 4, floatx4{0.f, 0.f, 0.f, 0.f});
       }
     }
     return;
@@ -261,8 +220,17 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
   // j_end.
   const int first0 = split * (split_keys / kWaveKeys);
   const int first = first0 + ws;
-  const int j_end = min((L + kWaveKeys - 1) / kWaveKeys, (split + 1) * (split_keys / kWaveKeys));
-  const int row_lim = min(L, j_end * kWaveKeys);  // a refill past the stream's last tile reads nothing
+  const int j_end = min(WIN ? reach.tiles : (L + kWaveKeys - 1) / kWaveKeys, (split + 1) * (split_keys / kWaveKeys));
+  const int row_lim = WIN ? L : min(L, j_end * kWaveKeys);  // a refill past the stream's last tile reads nothing
+  // First key of tile j (with a window, past the stream's last tile: a row that is never read).
+  auto tile_key = [&](int j) __attribute__((always_inline)) {
+    return !WIN ? j * kWaveKeys : j < j_end ? reach.start(j) : L;
+  };
+  // Whether some row sees key k, and whether every row sees the tile from key k on (but for the causal limit)
+  auto in_reach = [&](int k) __attribute__((always_inline)) { return !WIN || k >= reach.first_key || k < sinks; };
+  auto all_see = [&](int k) __attribute__((always_inline)) { return !WIN || k > L - 1 - window || k + kWaveKeys <= sinks; };
+  // Whether the row whose last key is lim sees key k <= lim
+  auto in_window = [&](int k, int lim) __attribute__((always_inline)) { return !WIN || k > lim - window || k < sinks; };
 
   // Every fetch issues the same loads (rows at or past kv_len, and tiles past
   // the stream's last, read out of range, as zero, with no traffic), so each
@@ -277,7 +245,7 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
   const uint32_t lane_col = (uint32_t)lane_chunk * 16;
   // this wave's rows of a tile: load u covers rows (h kLd + u) kRowsPerLoad + lane_row
   auto fetch = [&](int j, Stage<D, QG>& st) __attribute__((always_inline)) {
-    const int kb0 = j * kWaveKeys;
+    const int kb0 = tile_key(j);
 #pragma unroll
     for (int u = 0; u < kLd; ++u) {
       const int row = kb0 + (h * kLd + u) * GG::kRowsPerLoad + lane_row;
@@ -293,8 +261,8 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
   auto step = [&](int& j, Stage<D, QG>& st) __attribute__((always_inline)) {
     unsigned char* kst = lds + ws * kBufs * GG::kWaveBytes;
     unsigned char* vst = kst + GG::kSlotK;
-    const int kb0 = j * kWaveKeys;
-    const bool key_ok = lane < kWaveKeys && kb0 + lane < L && (mrow == nullptr || st.mbyte != 0u);
+    const int kb0 = tile_key(j);
+    const bool key_ok = lane < kWaveKeys && kb0 + lane < L && in_reach(kb0 + lane) && (mrow == nullptr || st.mbyte != 0u);
     const uint32_t vbits = (uint32_t)__ballot(key_ok) & 0xffffu;
     const bool all_rows = vbits == 0xffffu;  // wave-uniform
 #pragma unroll
@@ -314,7 +282,7 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
     const int jc = j;
     j = nx;
     if (jc >= j_end || rbase >= Mb) return;  // wave-uniform: past the stream's last tile, or no live rows
-    const bool full = vbits == 0xffffu && kb0 + kWaveKeys - 1 <= causal0;  // wave-uniform
+    const bool full = vbits == 0xffffu && kb0 + kWaveKeys - 1 <= causal0 && all_see(kb0);  // wave-uniform
     // ---- S^T = K Q^T (16 keys x 16 queries per block)
     floatx4 sacc[NQ];
 #pragma unroll
@@ -354,7 +322,7 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int kl = lg * 4 + e;
-            const bool vis = ((vbits >> kl) & 1u) && (kb0 + kl <= lim);
+            const bool vis = ((vbits >> kl) & 1u) && (kb0 + kl <= lim) && in_window(kb0 + kl, lim);
             s[e] = vis ? sacc[qg][e] * scale_log2 : kNegInf;
             mt = fmaxf(mt, s[e]);
           }
@@ -420,8 +388,9 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
     auto stage = [&](int j, Stage<D, QG>& st, int buf) __attribute__((always_inline)) {
       unsigned char* kd = kst + buf * GG::kWaveBytes;
       unsigned char* vd = kd + GG::kSlotK;
-      const int kb0 = j * kWaveKeys;
-      const bool key_ok = lane < kWaveKeys && j < j_end && kb0 + lane < L && (mrow == nullptr || st.mbyte != 0u);
+      const int kb0 = tile_key(j);
+      const bool key_ok =
+          lane < kWaveKeys && j < j_end && kb0 + lane < L && in_reach(kb0 + lane) && (mrow == nullptr || st.mbyte != 0u);
       const uint32_t vbits = (uint32_t)__ballot(key_ok) & 0xffffu;
       const bool all_rows = vbits == 0xffffu;  // wave-uniform
 #pragma unroll
@@ -446,7 +415,8 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
     fetch(jb, sb);
     __builtin_amdgcn_sched_barrier(0);
     if (j0 < j_end && rbase < Mb) {  // wave-uniform
-      const bool full = (vb[0] & vb[1]) == 0xffffu && j1 * kWaveKeys + kWaveKeys - 1 <= causal0;  // wave-uniform
+      const int kb[2] = {tile_key(j0), tile_key(j1)};
+      const bool full = (vb[0] & vb[1]) == 0xffffu && kb[1] + kWaveKeys - 1 <= causal0 && all_see(kb[0]) && all_see(kb[1]);  // wave-uniform
       floatx4 sacc[2][NQ];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -485,8 +455,8 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const int kl = lg * 4 + e % 4;
-              const int kb0 = (e < 4 ? j0 : j1) * kWaveKeys;
-              const bool vis = ((vb[e / 4] >> kl) & 1u) && (kb0 + kl <= lim);
+              const int k = kb[e / 4] + kl;
+              const bool vis = ((vb[e / 4] >> kl) & 1u) && (k <= lim) && in_window(k, lim);
               sc[e] = vis ? sacc[e / 4][qg][e % 4] * scale_log2 : kNegInf;
               mt = fmaxf(mt, sc[e]);
             }
@@ -580,247 +550,14 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
   }
   __syncthreads();
 
-  // ---- merge the four stream states of each query group (every wave and lane takes part)
-  using LL = Lds<D, NQ, QG>;
-  const int tg = tid - h * 64 * kWaves;                               // thread index in the group
-  float* slots = (float*)lds + h * kWaves * LL::kSlot;                  // [kWaves][MQ][kRowStride]
-  float* mlx = (float*)(lds + LL::kMl) + h * (kWaves + 1) * 2 * MQ;     // [kWaves][2][MQ]: each stream's (m, l)
-  float* mlf = mlx + kWaves * 2 * MQ;                                   // [2][MQ]: merged (M, L)
-  if (lg == 0) {
-#pragma unroll
-    for (int qg = 0; qg < NQ; ++qg) {
-      mlx[(ws * 2) * MQ + qg * 16 + l16] = m_run[qg];
-      mlx[(ws * 2 + 1) * MQ + qg * 16 + l16] = l_run[qg];
-    }
-  }
-  __syncthreads();
-  float cw[NQ];  // this stream's weight exp2(m_w - M) per row block
-#pragma unroll
-  for (int qg = 0; qg < NQ; ++qg) {
-    const int rl = qg * 16 + l16;
-    float M = kNegInf;
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) M = fmaxf(M, mlx[(v * 2) * MQ + rl]);
-    float Lsum = 0.f;
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-      const float c = M == kNegInf ? 0.f : exp2f(mlx[(v * 2) * MQ + rl] - M);
-      Lsum += c * mlx[(v * 2 + 1) * MQ + rl];
-    }
-    cw[qg] = M == kNegInf ? 0.f : exp2f(m_run[qg] - M);
-    if (ws == 0 && lg == 0) {
-      mlf[rl] = M;
-      mlf[MQ + rl] = Lsum;
-    }
-  }
-
-  // With a single split holding keys the result is final here, otherwise it
-  // is published as the split's partial.
-  const size_t pair = (size_t)(b * Hkv + g);
-  const int n_rec = (int)((size_t)n_splits * P) * R;  // records in the partial arrays
-  const __amdgpu_buffer_rsrc_t rs_o = partial_rsrc(part_o, (uint32_t)((size_t)n_rec * D * 4));
-  const __amdgpu_buffer_rsrc_t rs_ml = partial_rsrc(part_ml, (uint32_t)((size_t)n_rec * 8));
-  constexpr int kItemsP = (MQ * (LL::kDp / 4) + 64 * kWaves - 1) / (64 * kWaves);
-#pragma unroll
-  for (int pass = 0; pass < LL::kPasses; ++pass) {
-    __syncthreads();  // (m, l) exchange read / previous pass's slices consumed
-#pragma unroll
-    for (int qg = 0; qg < NQ; ++qg) {
-      const int rl = qg * 16 + l16;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const int col = db * 16 + lg * 4 - pass * LL::kDp;
-        if (col >= 0 && col < LL::kDp) *(floatx4*)(slots + (ws * MQ + rl) * LL::kRowStride + col) = o[db][qg] * cw[qg];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kItemsP; ++k) {
-      const int idx = tg + k * 64 * kWaves;
-      if (idx >= MQ * (LL::kDp / 4)) continue;
-      const int rl = idx / (LL::kDp / 4);
-      const int c4 = idx % (LL::kDp / 4);
-      const int r = rbase + rl;
-      if (r >= row_end) continue;
-      floatx4 sum = *(const floatx4*)(slots + rl * LL::kRowStride + c4 * 4);
-#pragma unroll
-      for (int v = 1; v < kWaves; ++v) sum += *(const floatx4*)(slots + (v * MQ + rl) * LL::kRowStride + c4 * 4);
-      const int col = pass * LL::kDp + c4 * 4;
-      if (ns == 1) {
-        const float Lr = mlf[MQ + rl];
-        const int i = r / G, hh = g * G + r % G;
-        *(floatx4*)(out + ((size_t)(b * (gmax + 1) + i) * Hq + hh) * D + col) =
-            (r < Mb && Lr > 0.f) ? sum * (1.f / Lr) : floatx4{0.f, 0.f, 0.f, 0.f};
-      } else if (r < Mb) {
-        const uint32_t rec = (uint32_t)((pair * n_splits + split) * R + r);
-        __builtin_amdgcn_raw_buffer_store_b128(sum, rs_o, (rec * D + col) * 4, 0, kDeviceCoherent);
-        if (pass == 0 && c4 == 0)
-          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, floatx2{mlf[rl], mlf[MQ + rl]}), rs_ml, rec * 8, 0, kDeviceCoherent);
-      }
-    }
-  }
-  if (ns == 1) return;
-
-  // ---- arrive: the last split of this job to finish merges all partials
-  stores_done();
-  __syncthreads();
-  __shared__ uint32_t last_flag;
-  if (tid == 0) {
-    uint32_t* cnt = counters + (size_t)job * kCounterStride;
-    const uint32_t before = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const bool last = before == (uint32_t)(ns - 1);
-    if (last) st_dev(cnt, 0u);  // every split of this job has arrived: reset for the next call
-    last_flag = last ? 1u : 0u;
-  }
-  __syncthreads();
-  if (last_flag == 0u) return;
-  __atomic_signal_fence(__ATOMIC_SEQ_CST);
-
-  // Merge: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over the splits, M
-  // their largest reference. Bound by the latency of the partials' device-coherent
-  // loads (one to two us a round trip, from another XCD's write), so as many as
-  // registers hold are in flight: first the first kGroup splits' outputs and
-  // every (m, l), then the remaining groups, with the weights from the (m, l) in
-  // LDS. (A running maximum over groups of four splits, their (m, l) beside the
-  // outputs, took 0.33 us per split at 24 rows of 128 columns; this takes
-  // 0.2.) Each thread owns kItems (row, 4 columns) items.
-  constexpr int kItems = (QG * MQ * (D / 4) + kT - 1) / kT;
-  // (registers: 32 to 96, fewer than the key loop's)
-  constexpr int kGroup = kItems >= 3 ? 4 : 8;
-  constexpr int kMlBlock = 64;  // splits whose references sit in LDS at once
-  constexpr int kRows = QG * MQ;
-  static_assert((2 + kMlBlock) * kRows * 4 <= Lds<D, NQ, QG>::kBytes, "the merge's exchange fits");
-  const int n_rows = row_end - row0;
-  const int n_items = n_rows * (D / 4);
-  float* mM = (float*)lds;           // [kRows] M
-  float* mD = mM + kRows;            // [kRows] denominators
-  float* mS = mD + kRows;            // [kMlBlock][kRows] m_s
-  const uint32_t rec0 = (uint32_t)(pair * n_splits * R);
-  const __amdgpu_buffer_rsrc_t rs_none = partial_rsrc(part_o, 0);
-  auto live_row = [&](int row) __attribute__((always_inline)) { return min(row0 + row, Mb - 1); };  // (rows past Mb hold no partial; their result is discarded)
-  // (past the splits: an empty resource, zeros without traffic)
-  auto sp_rsrc = [&](int sp, const __amdgpu_buffer_rsrc_t& rs) __attribute__((always_inline)) { return sp < ns ? rs : rs_none; };
-  auto fetch_o = [&](int sp0, floatx4 (&o2)[kGroup][kItems]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < kGroup; ++j)
-#pragma unroll
-      for (int k = 0; k < kItems; ++k) {
-        const int idx = min(tid + k * kT, n_items - 1);
-        const uint32_t rec = rec0 + (uint32_t)((sp0 + j) * R + live_row(idx / (D / 4)));
-        o2[j][k] = __builtin_amdgcn_raw_buffer_load_b128(sp_rsrc(sp0 + j, rs_o), (rec * D + (idx % (D / 4)) * 4) * 4, 0, kDeviceCoherent);
-      }
-  };
-  auto write_item = [&](int k, const floatx4& sum, float den) __attribute__((always_inline)) {
-    const int idx = tid + k * kT;
-    if (idx >= n_items) return;
-    const int r = row0 + idx / (D / 4);
-    const bool live = r < Mb && den > 0.f;
-    const floatx4 res = live ? sum * (1.f / den) : floatx4{0.f, 0.f, 0.f, 0.f};
-    const int i = r / G, hh = g * G + r % G;
-    *(floatx4*)(out + ((size_t)(b * (gmax + 1) + i) * Hq + hh) * D + (idx % (D / 4)) * 4) = res;
-  };
-  floatx4 o2[kGroup][kItems];
-  fetch_o(0, o2);
-  __builtin_amdgcn_sched_barrier(0);
-  constexpr int kFew = 4;
-  if (kItems <= 4 && ns <= kFew) {  // one round trip: every thread takes its rows' (m, l) itself (0.4 us less than through LDS)
-#pragma unroll
-    for (int k = 0; k < (kItems <= 4 ? kItems : 0); ++k) {
-      const int row = live_row(min(tid + k * kT, n_items - 1) / (D / 4));
-      floatx2 x[kFew];
-#pragma unroll
-      for (int j = 0; j < kFew; ++j)
-        x[j] = __builtin_bit_cast(floatx2, __builtin_amdgcn_raw_buffer_load_b64(sp_rsrc(j, rs_ml), (rec0 + (uint32_t)(j * R + row)) * 8, 0, kDeviceCoherent));
-      float M = kNegInf, den = 0.f;
-#pragma unroll
-      for (int j = 0; j < kFew; ++j) M = j < ns ? fmaxf(M, x[j].x) : M;
-      floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < kFew; ++j) {
-        const float wgt = j < ns && x[j].x != kNegInf ? exp2_hw(x[j].x - M) : 0.f;
-        den += x[j].y * wgt;
-        sum += o2[j][k] * wgt;
-      }
-      write_item(k, sum, den);
-    }
-    return;
-  }
-  // (m, l) of every split: four threads per row take the splits in turn
-  for (int row = tid / 4; row < n_rows; row += kT / 4) {
-    constexpr int kMl = 8;
-    float M = kNegInf, den = 0.f;
-    const uint32_t rec = rec0 + (uint32_t)live_row(row);
-    for (int sp0 = tid % 4; sp0 < ns; sp0 += 4 * kMl) {
-      floatx2 x[kMl];
-#pragma unroll
-      for (int j = 0; j < kMl; ++j)
-        x[j] = __builtin_bit_cast(floatx2, __builtin_amdgcn_raw_buffer_load_b64(
-                                               rs_ml, sp0 + 4 * j < ns ? (rec + (uint32_t)((sp0 + 4 * j) * R)) * 8 : kOutOfRange, 0, kDeviceCoherent));
-      float Mn = M;
-#pragma unroll
-      for (int j = 0; j < kMl; ++j) Mn = sp0 + 4 * j < ns ? fmaxf(Mn, x[j].x) : Mn;
-      den = Mn == kNegInf ? 0.f : den * exp2_hw(M - Mn);
-#pragma unroll
-      for (int j = 0; j < kMl; ++j) {
-        const int sp = sp0 + 4 * j;
-        if (sp < ns) {
-          if (Mn != kNegInf) den += x[j].y * exp2_hw(x[j].x - Mn);
-          if (sp < kMlBlock) mS[sp * kRows + row] = x[j].x;
-        }
-      }
-      M = Mn;
-    }
-    // the row's four threads (a quad): (M, den) over all splits
-#pragma unroll
-    for (int d = 1; d < 4; d <<= 1) {
-      const float Mo = d == 1 ? perm_f32<dpp::kXor1>(M) : perm_f32<dpp::kXor2>(M);
-      const float Do = d == 1 ? perm_f32<dpp::kXor1>(den) : perm_f32<dpp::kXor2>(den);
-      const float Mn = fmaxf(M, Mo);
-      den = Mn == kNegInf ? 0.f : den * exp2_hw(M - Mn) + Do * exp2_hw(Mo - Mn);
-      M = Mn;
-    }
-    if (tid % 4 == 0) {
-      mM[row] = M;
-      mD[row] = den;
-    }
-  }
-  floatx4 acc[kItems];
-#pragma unroll
-  for (int k = 0; k < kItems; ++k) acc[k] = floatx4{0.f, 0.f, 0.f, 0.f};
-  __syncthreads();
-  for (int b0 = 0; b0 < ns; b0 += kMlBlock) {
-    if (b0 > 0) {  // the next block's references
-      __syncthreads();
-      for (int i = tid; i < min(ns - b0, kMlBlock) * n_rows; i += kT) {
-        const int sp = i / n_rows, row = i % n_rows;
-        mS[sp * kRows + row] = __builtin_bit_cast(floatx2, __builtin_amdgcn_raw_buffer_load_b64(
-                                                             rs_ml, (rec0 + (uint32_t)((b0 + sp) * R + live_row(row))) * 8, 0, kDeviceCoherent)).x;
-      }
-      __syncthreads();
-    }
-    const int b1 = min(ns, b0 + kMlBlock);
-    for (int sp0 = b0; sp0 < b1; sp0 += kGroup) {
-      if (sp0 > 0) fetch_o(sp0, o2);
-#pragma unroll
-      for (int k = 0; k < kItems; ++k) {
-        const int row = min(tid + k * kT, n_items - 1) / (D / 4);
-        const float M = mM[row];
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j) {
-          const float m = mS[(sp0 + j < b1 ? sp0 + j - b0 : 0) * kRows + row];
-          const float wgt = sp0 + j < b1 && m != kNegInf ? exp2_hw(m - M) : 0.f;
-          acc[k] += o2[j][k] * wgt;
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < kItems; ++k) write_item(k, acc[k], mD[min(tid + k * kT, n_items - 1) / (D / 4)]);
+  const JobRows J{row0, row_end, Mb, R, split, ns, n_splits, job, P, (size_t)(b * Hkv + g)};
+  merge_and_store<D, NQ, QG, Lds<D, NQ, QG>::kBytes, WIN>(
+      lds, o, m_run, l_run, J, part_o, part_ml, counters, store);
 }
 
 typedef void (*SplitKernel)(const uint16_t*, const uint16_t*, const uint16_t*, const uint8_t*,
-                            const int32_t*, const int32_t*, float*, float*, float*, uint32_t*,
-                            const int32_t*, int, int, int, int, int, float, int, int, int, int32_t*);
+                            const int32_t*, const int32_t*, void*, bool, float*, float*, uint32_t*,
+                            const int32_t*, int, int, int, int, int, int, int, float, int, int, int, int32_t*);
 
 // The dispatch order of the split workgroups when there are more than fit on
 // the device at once (one workgroup of kOrderThreads): every job (sequence,
@@ -836,7 +573,8 @@ constexpr int kOrderKept = 4;        // buckets a thread keeps between the two p
 static_assert(kOrderThreads == kOrderBuckets, "one scan element per thread");
 __global__ void __launch_bounds__(kOrderThreads)
 attn_order_kernel(const int32_t* __restrict__ kv_len, const int32_t* __restrict__ gamma, int B, int gmax,
-                  int Hkv, int q_chunks, int L_cap, int split_keys, int n_splits, int32_t* __restrict__ order) {
+                  int Hkv, int q_chunks, int L_cap, int window, int sinks, int tile, int split_keys, int n_splits,
+                  int32_t* __restrict__ order) {
   __shared__ int cnt[kOrderBuckets];
   __shared__ int wsum[kOrderThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -846,7 +584,12 @@ attn_order_kernel(const int32_t* __restrict__ kv_len, const int32_t* __restrict_
     const int b = item / n_splits, sp = item % n_splits;
     const int gam = gamma[b], L = kv_len[b];
     const bool valid = gam >= 0 && gam <= gmax && L >= gam + 1 && L <= L_cap;
-    const int len = valid ? min(L, (sp + 1) * split_keys) - sp * split_keys : 0;
+    int keys = L;  // with a window, the keys of the tiles in reach
+    if (window > 0 && valid) {
+      if (tile == 16) keys = Reach<16>(L - gam - 1, L, window, sinks).tiles * 16;
+      else keys = Reach<32>(L - gam - 1, L, window, sinks).tiles * 32;
+    }
+    const int len = valid ? min(keys, (sp + 1) * split_keys) - sp * split_keys : 0;
     return len <= 0 ? 0 : min((len + kWaveKeys - 1) / kWaveKeys, kOrderBuckets - 1);
   };
   cnt[tid] = 0;
@@ -894,27 +637,30 @@ attn_order_kernel(const int32_t* __restrict__ kv_len, const int32_t* __restrict_
   for (int item = tid + kOrderKept * kOrderThreads; item < n_items; item += kOrderThreads) place(item, bucket(item));
 }
 
-template <int D, bool FOLLOW>
+template <int D, bool FOLLOW, bool WIN>
 SplitKernel pick_split(int nq, int qg, int q_chunks) {
   if (qg == 1) {
     switch (nq) {
-      case 1: return attn_split_kernel<D, 1, 1, true, FOLLOW>;
-      case 2: return attn_split_kernel<D, 2, 1, true, FOLLOW>;
-      default: return attn_split_kernel<D, 3, 1, true, FOLLOW>;
+      case 1: return attn_split_kernel<D, 1, 1, true, FOLLOW, WIN>;
+      case 2: return attn_split_kernel<D, 2, 1, true, FOLLOW, WIN>;
+      default: return attn_split_kernel<D, 3, 1, true, FOLLOW, WIN>;
     }
   }
-  if (nq == 2) return attn_split_kernel<D, 2, 2, true, FOLLOW>;
-  return q_chunks == 1 ? attn_split_kernel<D, 3, 2, true, FOLLOW> : attn_split_kernel<D, 3, 2, false, FOLLOW>;
+  if (nq == 2) return attn_split_kernel<D, 2, 2, true, FOLLOW, WIN>;
+  return q_chunks == 1 ? attn_split_kernel<D, 3, 2, true, FOLLOW, WIN> : attn_split_kernel<D, 3, 2, false, FOLLOW, WIN>;
 }
 
+template <bool WIN>
 SplitKernel pick_split(int D, int nq, int qg, int q_chunks, bool follow) {
-  if (follow) return D == 64 ? pick_split<64, true>(nq, qg, q_chunks) : pick_split<128, true>(nq, qg, q_chunks);
-  return D == 64 ? pick_split<64, false>(nq, qg, q_chunks) : pick_split<128, false>(nq, qg, q_chunks);
+  if (follow) return D == 64 ? pick_split<64, true, WIN>(nq, qg, q_chunks) : pick_split<128, true, WIN>(nq, qg, q_chunks);
+  return D == 64 ? pick_split<64, false, WIN>(nq, qg, q_chunks) : pick_split<128, false, WIN>(nq, qg, q_chunks);
 }
 
 }  // namespace
 
-int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap, AttentionPlan* plan) {
+int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_rows, int window, int sinks,
+                   AttentionPlan* plan) {
+  const int L_cap = reach_cap(kWaveKeys, gamma_max, cache_rows, window, sinks);  // keys of a sequence at most
   const int G = Hq / Hkv;
   const int R = G * (gamma_max + 1);
   // Up to 48 rows: one four-wave group of ceil(R / 16) row blocks. Beyond:
@@ -932,7 +678,8 @@ int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap, Atte
   const int cus = device_cu_count();
   if (cus <= 0) return SR_ELAUNCH;
   const int threads = plan->qg == 1 ? Shape<1>::kThreads : Shape<kMaxQG>::kThreads;
-  const int per_cu = resident_per_cu((const void*)pick_split(D, plan->nq, plan->qg, plan->q_chunks, false), threads, 0);
+  const int per_cu = resident_per_cu((const void*)(window > 0 ? pick_split<true>(D, plan->nq, plan->qg, plan->q_chunks, false)
+                                                                 : pick_split<false>(D, plan->nq, plan->qg, plan->q_chunks, false)), threads, 0);
   const long pairs = (long)B * Hkv * plan->q_chunks;
   const long target = (long)cus * per_cu;
   // Splits: the count, up to one workgroup per CU, whose time is least for
@@ -1015,10 +762,18 @@ int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap, Atte
   return SR_OK;
 }
 
+int launch_attention_order(const int32_t* kv_len, const int32_t* gamma, int B, int gamma_max, int Hkv, int q_chunks,
+                           int L_cap, int window, int sinks, int tile, int split_keys, int n_splits, int32_t* order,
+                           hipStream_t stream) {
+  hipLaunchKernelGGL(attn_order_kernel, dim3(1), dim3(kOrderThreads), 0, stream, kv_len, gamma, B, gamma_max, Hkv,
+                     q_chunks, L_cap, window, sinks, tile, split_keys, n_splits, order);
+  return hipGetLastError() == hipSuccess ? SR_OK : SR_ELAUNCH;
+}
+
 int launch_verify_attention(const void* q, const void* k_cache, const void* v_cache,
                             const uint8_t* cache_mask, const int32_t* kv_len,
-                            const int32_t* gamma, float* out, int B, int gamma_max, int Hq,
-                            int Hkv, int D, int L_cap, float scale, void* workspace,
+                            const int32_t* gamma, void* out, bool out_bf16, int B, int gamma_max, int Hq,
+                            int Hkv, int D, int L_cap, int window, int sinks, float scale, void* workspace,
                             const AttentionPlan& plan, int32_t* status, hipStream_t stream) {
   const int G = Hq / Hkv;
   const int R = G * (gamma_max + 1);
@@ -1028,17 +783,16 @@ int launch_verify_attention(const void* q, const void* k_cache, const void* v_ca
   dim3 grid((unsigned)((long)plan.n_splits * plan.q_chunks * B * Hkv));
   const int threads = plan.qg == 1 ? Shape<1>::kThreads : Shape<kMaxQG>::kThreads;
   int32_t* order = plan.ordered ? (int32_t*)((char*)workspace + plan.order_offset) : nullptr;
-  if (order) {
-    hipLaunchKernelGGL(attn_order_kernel, dim3(1), dim3(kOrderThreads), 0, stream, kv_len, gamma, B, gamma_max,
-                       Hkv, plan.q_chunks, L_cap, plan.split_keys, plan.n_splits, order);
-    if (hipGetLastError() != hipSuccess) return SR_ELAUNCH;
-  }
-  hipLaunchKernelGGL(pick_split(D, plan.nq, plan.qg, plan.q_chunks, plan.follow != 0), grid, dim3(threads), 0, stream,
-                     (const uint16_t*)q, (const uint16_t*)k_cache, (const uint16_t*)v_cache,
-                     cache_mask, kv_len, gamma, out, part_o, part_ml, counters, order, B, gamma_max, Hq,
-                     Hkv, L_cap, scale * kLog2e, plan.split_keys, plan.n_splits, plan.q_chunks, status);
-  if (hipGetLastError() != hipSuccess) return SR_ELAUNCH;
-  return SR_OK;
+  if (order && launch_attention_order(kv_len, gamma, B, gamma_max, Hkv, plan.q_chunks, L_cap, window, sinks, kWaveKeys,
+                                      plan.split_keys, plan.n_splits, order, stream) != SR_OK)
+    return SR_ELAUNCH;
+  const SplitKernel kernel = window > 0 ? pick_split<true>(D, plan.nq, plan.qg, plan.q_chunks, plan.follow != 0)
+                                        : pick_split<false>(D, plan.nq, plan.qg, plan.q_chunks, plan.follow != 0);
+  hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, (const uint16_t*)q, (const uint16_t*)k_cache,
+                     (const uint16_t*)v_cache, cache_mask, kv_len, gamma, out, out_bf16, part_o, part_ml, counters,
+                     order, B, gamma_max, Hq, Hkv, L_cap, window, sinks, scale * kLog2e, plan.split_keys, plan.n_splits,
+                     plan.q_chunks, status);
+  return hipGetLastError() == hipSuccess ? SR_OK : SR_ELAUNCH;
 }
 
 }  // namespace sr

@@ -1,0 +1,415 @@
+// Verification attention over a K/V cache held in 4 bits (gfx950): the
+// attention of the new rows (Section 2.2 step 2; Section 4.4, Eq. 8), with or
+// without a window, over e2m1 codes with a power of two per 32 elements of a row.
+//
+// Work decomposition as over a bf16 cache: a workgroup of four waves takes one
+// (sequence, kv head, query chunk, key split), the waves deal the split's tiles
+// of 32 keys among themselves, and their states merge through LDS, those of
+// several splits through the workspace.
+//
+// A code times its power is exact in bf16, so both products run on bf16 MFMA and
+// the only roundings are those of the bf16 attention (P, and the output's).
+// The hardware widens two codes per instruction and scales them on the way
+// (v_cvt_scalef32_pk_bf16_fp4). Per 32-key tile of a wave, lane (l16, lg):
+//   * K: lane l16 of quarter lg takes a quarter of the key's row (D/4 codes, one
+//     16-byte load at D = 128), which all lie under one power. Widened, they are
+//     the A operand of S^T = K Q^T as they stand: the contraction over the head
+//     dimension takes its elements in the order (ks, lg, e) -> lg D/4 + 8 ks + e,
+//     and the query rows, which stay in registers, are held in the same order. K
+//     never passes through LDS.
+//   * V: the same load, widened and written to the wave's own LDS slot row by row
+//     (rows that no query sees as zeros), to come back transposed
+//     (ds_read_b64_tr_b16) as the A operand of O^T += V^T P^T over 32 keys. The
+//     16-byte chunks of a row are permuted by the row's number, so that neither
+//     the writes (eight rows at a time) nor the transposing reads (four) meet in
+//     a bank.
+//   * softmax as over bf16: a row's reference is raised only when a tile exceeds
+//     it by more than 2^8, P rounds to bf16.
+
+#include "attention_common.h"
+
+namespace sr {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 32;   // keys per tile of a wave
+constexpr int kRing4 = 2;   // tiles in flight per wave
+constexpr int kMaxNQ4 = 3;  // 16-row query blocks per wave: more than 48 rows go to further query chunks
+
+template <int D, int NQ>
+struct Lds4 {
+  static constexpr int kRow = D * 2;               // bytes of a widened V row
+  static constexpr int kSlot = kTile * kRow;       // per wave
+  static constexpr int kStage = kWaves * kSlot;
+  static constexpr int kComb = MergeLds<D, NQ, 1>::kComb;
+  static constexpr int kBytes = kStage > kComb ? kStage : kComb;
+};
+
+// Eight codes (one dword) times 2^(p - 127), `scale` that power as a float.
+__device__ __forceinline__ u32x4 widen(uint32_t codes, float scale) {
+  u32x4 v;
+  v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+  v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+  v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+  v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+  return v;
+}
+
+// Where 16-byte chunk c of V row r sits in its row.
+__device__ __forceinline__ int chunk_at(int c, int r) { return c ^ (((r & 3) << 1) | ((r >> 2) & 1)); }
+
+template <int D>
+struct Stage4 {  // a 32-key tile in flight: rows u 16 + l16
+  uint32_t k[2][D / 32], v[2][D / 32];
+  uint32_t kp[2], vp[2];
+  uint32_t mbyte;  // validity byte of key (lane mod 32)
+};
+
+struct Kv4Args {
+  const uint16_t* q;
+  const uint8_t *kc, *kp, *vc, *vp;
+  const uint8_t* mask;
+  const int32_t *kv_len, *gamma;
+  void* out;
+  bool out_bf16;
+  float *part_o, *part_ml;
+  uint32_t* counters;
+  const int32_t* order;
+  int B, gmax, Hq, Hkv, L_cap, window, sinks;
+  float scale_log2;
+  int split_keys, n_splits, q_chunks;
+  int32_t* status;
+};
+
+template <int D, int NQ, bool NT>
+__global__ void __launch_bounds__(64 * kWaves, NQ == 1 ? 3 : 2)
+attn_kv4_kernel(Kv4Args a) {
+  constexpr int MQ = 16 * NQ;
+  constexpr int DB = D / 16;
+  constexpr int KS = D / 32;   // contraction steps of 32, dwords of codes per lane and row
+  constexpr int EL = D / 4;    // elements per lane and row
+  constexpr int kT = 64 * kWaves;
+  using LL = Lds4<D, NQ>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[LL::kBytes];
+
+  const int P = a.B * a.Hkv;
+  const int rest = (int)(blockIdx.x / (unsigned)P);
+  const int code = a.order ? __builtin_amdgcn_readfirstlane(a.order[blockIdx.x])
+                           : ((int)(blockIdx.x % (unsigned)P) * a.q_chunks + rest / a.n_splits) * a.n_splits +
+                                 (a.n_splits - 1 - rest % a.n_splits);
+  const int split = code % a.n_splits;
+  const int job = code / a.n_splits;
+  const int qc = job % a.q_chunks;
+  const int pair_id = job / a.q_chunks;
+  const int g = pair_id % a.Hkv;
+  const int b = pair_id / a.Hkv;
+  const int G = a.Hq / a.Hkv;
+  const int R = G * (a.gmax + 1);
+  const int gam = a.gamma[b];
+  const int L = a.kv_len[b];
+  const bool valid = gam >= 0 && gam <= a.gmax && L >= gam + 1 && L <= a.L_cap;
+  if (!valid && split == 0 && qc == 0 && g == 0 && threadIdx.x == 0 && a.status) {
+    atomicOr(a.status, (gam < 0 || gam > a.gmax) ? SR_ST_GAMMA : SR_ST_KVLEN);
+  }
+  const int row0 = qc * MQ;
+  const int row_end = min(R, row0 + MQ);
+  const int Mb = valid ? G * (gam + 1) : 0;
+  const int window = a.window > 0 ? a.window : 0x7fffffff;
+  const int sinks = a.sinks;
+  const int causal0 = valid ? L - gam - 1 : 0;  // cache position of new row 0
+  const Reach<kTile> reach(causal0, valid ? L : 0, window, sinks);
+  const int tiles_per = a.split_keys / kTile;
+  const int ns = (reach.tiles + tiles_per - 1) / tiles_per;  // splits that hold keys
+  const bool work = row0 < Mb && split < ns;
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int ws = wave_id();  // key stream
+  const int l16 = lane & 15;
+  const int lg = lane >> 4;
+
+  // Four columns of output row r (bf16: rounded once, from the 32-bit sums).
+  auto store = [&](int r, int col, const floatx4& x) __attribute__((always_inline)) {
+    const int i = r / G, hh = g * G + r % G;
+    const size_t at = ((size_t)(b * (a.gmax + 1) + i) * a.Hq + hh) * D + col;
+    if (a.out_bf16) *(u32x2*)((uint16_t*)a.out + at) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    else *(floatx4*)((float*)a.out + at) = x;
+  };
+  if (!work) {
+    // Split 0 of a query chunk without live rows (or of an invalid sequence) writes those rows as zero.
+    if (split == 0)
+      for (int idx = tid; idx < (row_end - row0) * (D / 4); idx += kT)
+        store(row0 + idx / (D / 4), idx % (D / 4) * 4, floatx4{0.f, 0.f, 0.f, 0.f});
+    return;
+  }
+
+  // slabs of (b, g) as buffer resources: 32-bit row offsets
+  const size_t slab = ((size_t)b * a.Hkv + g) * (size_t)a.L_cap;
+  const __amdgpu_buffer_rsrc_t rkc = make_rsrc(a.kc + slab * (D / 2), (size_t)a.L_cap * (D / 2));
+  const __amdgpu_buffer_rsrc_t rvc = make_rsrc(a.vc + slab * (D / 2), (size_t)a.L_cap * (D / 2));
+  const __amdgpu_buffer_rsrc_t rkp = make_rsrc(a.kp + slab * (D / 32), (size_t)a.L_cap * (D / 32));
+  const __amdgpu_buffer_rsrc_t rvp = make_rsrc(a.vp + slab * (D / 32), (size_t)a.L_cap * (D / 32));
+  const uint8_t* mrow = a.mask ? a.mask + (size_t)b * a.L_cap : nullptr;
+  const uint8_t* mload = mrow ? mrow : a.kc + slab * (D / 2);
+
+  floatx4 o[DB][NQ];
+  float m_run[NQ], l_run[NQ];
+#pragma unroll
+  for (int qg = 0; qg < NQ; ++qg) {
+    m_run[qg] = kNegInf;
+    l_run[qg] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db][qg] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // The split's tiles [t0, t_end), dealt round-robin to the streams.
+  const int t0 = split * tiles_per;
+  const int t_end = min(reach.tiles, t0 + tiles_per);
+  auto tile_key = [&](int t) __attribute__((always_inline)) { return t < t_end ? reach.start(t) : L; };
+  constexpr int kPolicy = NT ? kStreamLoad : 0;
+  auto fetch = [&](int t, Stage4<D>& st) __attribute__((always_inline)) {
+    const int kb0 = tile_key(t);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int row = kb0 + u * 16 + l16;
+      const uint32_t off = row < L ? (uint32_t)row * (D / 2) + (uint32_t)lg * (EL / 2) : kOutOfRange;
+      const uint32_t poff = row < L ? (uint32_t)row * (D / 32) + (uint32_t)(lg * EL / 32) : kOutOfRange;
+      if constexpr (D == 128) {
+        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rkc, off, 0, kPolicy));
+        const u32x4 y = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rvc, off, 0, kPolicy));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st.k[u][e] = x[e], st.v[u][e] = y[e];
+      } else {
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rkc, off, 0, kPolicy));
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rvc, off, 0, kPolicy));
+        st.k[u][0] = x[0], st.k[u][1] = x[1], st.v[u][0] = y[0], st.v[u][1] = y[1];
+      }
+      st.kp[u] = __builtin_amdgcn_raw_buffer_load_b8(rkp, poff, 0, kPolicy);
+      st.vp[u] = __builtin_amdgcn_raw_buffer_load_b8(rvp, poff, 0, kPolicy);
+    }
+    st.mbyte = mload[min(kb0 + (lane & (kTile - 1)), L - 1)];
+  };
+
+  // This lane's part of the query rows: qf[qg][ks] holds Q[qg 16 + l16][lg EL + 8 ks ..].
+  bf16x8 qf[NQ][KS];
+#pragma unroll
+  for (int qg = 0; qg < NQ; ++qg) {
+    const int r = row0 + qg * 16 + l16;
+    const int rc = min(r, Mb - 1), i = rc / G, hh = g * G + rc % G;
+    const uint16_t* src = a.q + ((size_t)(b * (a.gmax + 1) + i) * a.Hq + hh) * D + lg * EL;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4 x = *(const u32x4*)(src + ks * 8);
+      qf[qg][ks] = __builtin_bit_cast(bf16x8, r < Mb ? x : u32x4{0u, 0u, 0u, 0u});
+    }
+  }
+  unsigned char* slot = lds + ws * LL::kSlot;
+
+  auto step = [&](int& t, Stage4<D>& st) __attribute__((always_inline)) {
+    const int kb0 = tile_key(t);
+    const int key = kb0 + (lane & (kTile - 1));
+    const bool key_ok = lane < kTile && key < L && (key >= reach.first_key || key < sinks) &&
+                        (mrow == nullptr || st.mbyte != 0u);
+    const uint32_t vbits = (uint32_t)__ballot(key_ok);  // keys that some row may see
+    // ---- V to LDS
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bool seen = (vbits >> (u * 16 + l16)) & 1u;
+      const float scale = __uint_as_float(seen ? st.vp[u] << 23 : 0u);
+      const int r = u * 16 + l16;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        *(u32x4*)(slot + r * LL::kRow + chunk_at(lg * KS + ks, r) * 16) = widen(seen ? st.v[u][ks] : 0u, scale);
+    }
+    // ---- S^T = K Q^T
+    floatx4 sacc[2][NQ];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const float scale = __uint_as_float(st.kp[u] << 23);
+#pragma unroll
+      for (int qg = 0; qg < NQ; ++qg) sacc[u][qg] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 ka = __builtin_bit_cast(bf16x8, widen(st.k[u][ks], scale));
+#pragma unroll
+        for (int qg = 0; qg < NQ; ++qg)
+          sacc[u][qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[qg][ks], sacc[u][qg], 0, 0, 0);
+      }
+    }
+    wave_lds_sync();
+    t += kRing4 * kWaves;
+    __builtin_amdgcn_sched_barrier(0);
+    fetch(t, st);
+    __builtin_amdgcn_sched_barrier(0);
+    // ---- mask, online softmax, P in bf16 (lane: keys u 16 + lg 4 + e of query l16)
+    const bool full = vbits == 0xffffffffu && kb0 + kTile - 1 <= causal0 &&
+                      (kb0 > L - 1 - window || kb0 + kTile <= sinks);  // wave-uniform
+    bf16x8 pb[NQ];
+#pragma unroll
+    for (int qg = 0; qg < NQ; ++qg) {
+      pb[qg] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+      if (row0 + qg * 16 < Mb) {
+        const int r = row0 + qg * 16 + l16;
+        float s[8];
+        float mt = kNegInf;
+        if (full) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            s[e] = sacc[e / 4][qg][e % 4];
+            mt = fmaxf(mt, s[e]);
+          }
+          mt *= a.scale_log2;
+        } else {
+          const int lim = r < Mb ? causal0 + r / G : -1;  // last key this query row sees
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int kl = (e / 4) * 16 + lg * 4 + e % 4;
+            const int k = kb0 + kl;
+            const bool vis = ((vbits >> kl) & 1u) && k <= lim && (k > lim - window || k < sinks);
+            s[e] = vis ? sacc[e / 4][qg][e % 4] * a.scale_log2 : kNegInf;
+            mt = fmaxf(mt, s[e]);
+          }
+        }
+        mt = max_across_rows(mt);
+        const bool grow = mt > m_run[qg] + kLazy;
+        const float mref = grow ? mt : m_run[qg];
+        const float alpha = m_run[qg] == mref ? 1.f : exp2_hw(m_run[qg] - mref);
+        const float mr = mref == kNegInf ? 0.f : mref;  // (-inf: no key of the row so far)
+        float pk[8];
+        float ls = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          pk[e] = exp2_hw(full ? fmaf(s[e], a.scale_log2, -mr) : s[e] - mr);
+          ls += pk[e];
+        }
+        ls = sum_across_rows(ls);
+        l_run[qg] = l_run[qg] * alpha + ls;
+        m_run[qg] = mref;
+        if (__ballot(grow) != 0ull) {
+#pragma unroll
+          for (int db = 0; db < DB; ++db) o[db][qg] *= alpha;
+        }
+        pb[qg] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(pk[0], pk[1]), pack_bf16x2(pk[2], pk[3]),
+                                                  pack_bf16x2(pk[4], pk[5]), pack_bf16x2(pk[6], pk[7])});
+      }
+    }
+    // ---- O^T += V^T P^T over the 32 keys: contraction slot lg 8 + e is key
+    // lg 4 + e (e < 4) or 16 + lg 4 + e - 4, as the scores lie in the registers
+    const int vr = lg * 4 + (l16 >> 2);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const unsigned char* p0 = slot + vr * LL::kRow + chunk_at(db * 2 + ((l16 & 3) >> 1), vr) * 16 + (l16 & 1) * 8;
+      const shortx4 va0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p0);
+      const shortx4 va1 =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(p0 + 16 * LL::kRow));
+      const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(va0, va1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int qg = 0; qg < NQ; ++qg)
+        o[db][qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[qg], o[db][qg], 0, 0, 0);
+    }
+    wave_lds_sync();  // this tile's LDS reads are issued before the slot is rewritten
+  };
+
+  __builtin_amdgcn_sched_barrier(0);
+  Stage4<D> ring[kRing4];
+  int tr[kRing4];
+#pragma unroll
+  for (int r = 0; r < kRing4; ++r) {
+    tr[r] = t0 + ws + r * kWaves;
+    fetch(tr[r], ring[r]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // (a step past the stream's last tile reads nothing and adds nothing)
+  while (tr[0] < t_end) {
+#pragma unroll
+    for (int r = 0; r < kRing4; ++r) step(tr[r], ring[r]);
+  }
+  __syncthreads();
+
+  const JobRows J{row0, row_end, Mb, R, split, ns, a.n_splits, job, P, (size_t)(b * a.Hkv + g)};
+  merge_and_store<D, NQ, 1, LL::kBytes, true>(lds, o, m_run, l_run, J, a.part_o, a.part_ml, a.counters, store);
+}
+
+typedef void (*Kv4Kernel)(Kv4Args);
+
+template <int D>
+Kv4Kernel pick_kv4(int nq, bool nt) {
+  switch (nq) {
+    case 1: return nt ? attn_kv4_kernel<D, 1, true> : attn_kv4_kernel<D, 1, false>;
+    case 2: return nt ? attn_kv4_kernel<D, 2, true> : attn_kv4_kernel<D, 2, false>;
+    default: return nt ? attn_kv4_kernel<D, 3, true> : attn_kv4_kernel<D, 3, false>;
+  }
+}
+Kv4Kernel pick_kv4(int D, int nq, int q_chunks) {
+  return D == 64 ? pick_kv4<64>(nq, q_chunks == 1) : pick_kv4<128>(nq, q_chunks == 1);
+}
+
+}  // namespace
+
+int attention_kv4_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_rows, int window, int sinks,
+                       AttentionPlan* plan) {
+  const int L = reach_cap(kTile, gamma_max, cache_rows, window, sinks);  // keys of a sequence at most
+  const int R = Hq / Hkv * (gamma_max + 1);
+  plan->qg = 1;
+  plan->q_chunks = (R + 16 * kMaxNQ4 - 1) / (16 * kMaxNQ4);
+  plan->nq = ((R + plan->q_chunks - 1) / plan->q_chunks + 15) / 16;
+  const int cus = device_cu_count();
+  if (cus <= 0) return SR_ELAUNCH;
+  const int per_cu = resident_per_cu((const void*)pick_kv4(D, plan->nq, plan->q_chunks), 64 * kWaves, 0);
+  const long pairs = (long)B * Hkv * plan->q_chunks;
+  const long target = (long)cus * per_cu;
+  // Splits: the count, up to two workgroups per CU, whose time is least, in
+  // units of a key's time in a workgroup: the keys of a split times the workgroups
+  // that the busiest CU gets, plus the merge of each split's partial.
+  constexpr long kPerSplit = 64;
+  const long most = (2L * cus + pairs - 1) / pairs;
+  long splits = 1, best = 0;
+  for (long n = 1; n <= most; ++n) {
+    const long t = (pairs * n + cus - 1) / cus * ((L + n - 1) / n) + (n > 1 ? n * kPerSplit : 0);
+    if (n == 1 || t < best) best = t, splits = n;
+  }
+  const long max_splits = (L + kTile - 1) / kTile;
+  if (splits > max_splits) splits = max_splits;
+  // Offsets into the partial arrays are 32-bit (buffer addressing): below 2^31 bytes.
+  const long max_by_offset = 0x7fffffffL / ((long)D * 4 * B * Hkv * R);
+  if (splits > max_by_offset) splits = max_by_offset > 1 ? max_by_offset : 1;
+  int sk = (int)((L + splits - 1) / splits);
+  sk = (sk + kTile - 1) / kTile * kTile;
+  plan->split_keys = sk;
+  plan->n_splits = (L + sk - 1) / sk;
+  plan->follow = 0;
+  // [arrival counters, one per 128-byte line][partial o][partial (m, l)][order]
+  const size_t counters = (size_t)pairs * kCounterStride * sizeof(uint32_t);
+  plan->part_offset = counters;
+  size_t bytes = plan->n_splits > 1 ? counters + (size_t)B * Hkv * plan->n_splits * R * (D + 2) * sizeof(float) : 0;
+  const long n_jobs = (long)plan->n_splits * pairs;
+  plan->ordered = n_jobs > target ? 1 : 0;
+  plan->order_offset = (bytes + 15) / 16 * 16;
+  if (plan->ordered) bytes = plan->order_offset + (size_t)n_jobs * sizeof(int32_t);
+  plan->workspace_bytes = bytes;
+  return SR_OK;
+}
+
+int launch_attention_kv4(const void* q, const void* k_codes, const void* k_powers, const void* v_codes,
+                         const void* v_powers, const uint8_t* cache_mask, const int32_t* kv_len, const int32_t* gamma,
+                         void* out, bool out_bf16, int B, int gamma_max, int Hq, int Hkv, int D, int L_cap, int window,
+                         int sinks, float scale, void* workspace, const AttentionPlan& plan, int32_t* status,
+                         hipStream_t stream) {
+  const int R = Hq / Hkv * (gamma_max + 1);
+  float* part_o = workspace ? (float*)((char*)workspace + plan.part_offset) : nullptr;
+  float* part_ml = part_o ? part_o + (size_t)B * Hkv * plan.n_splits * R * D : nullptr;
+  int32_t* order = plan.ordered ? (int32_t*)((char*)workspace + plan.order_offset) : nullptr;
+  if (order && launch_attention_order(kv_len, gamma, B, gamma_max, Hkv, plan.q_chunks, L_cap, window, sinks, kTile,
+                                      plan.split_keys, plan.n_splits, order, stream) != SR_OK)
+    return SR_ELAUNCH;
+  const Kv4Args a{(const uint16_t*)q, (const uint8_t*)k_codes, (const uint8_t*)k_powers, (const uint8_t*)v_codes,
+                  (const uint8_t*)v_powers, cache_mask, kv_len, gamma, out, out_bf16, part_o, part_ml,
+                  (uint32_t*)workspace, order, B, gamma_max, Hq, Hkv, L_cap, window, sinks, scale * kLog2e,
+                  plan.split_keys, plan.n_splits, plan.q_chunks, status};
+  const dim3 grid((unsigned)((long)plan.n_splits * plan.q_chunks * B * Hkv));
+  hipLaunchKernelGGL(pick_kv4(D, plan.nq, plan.q_chunks), grid, dim3(64 * kWaves), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SR_OK : SR_ELAUNCH;
+}
+
+}  // namespace sr

@@ -271,13 +271,26 @@ struct AttentionPlan {
   size_t workspace_bytes;
 };
 
-int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap, AttentionPlan* plan);
+// window 0: all keys, else the last `window` positions of each row and the first `sinks`
+int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap, int window, int sinks, AttentionPlan* plan);
 
+// (an output in bf16 only with a window)
 int launch_verify_attention(const void* q, const void* k_cache, const void* v_cache,
                             const uint8_t* cache_mask, const int32_t* kv_len,
-                            const int32_t* gamma, float* out, int B, int gamma_max, int Hq,
-                            int Hkv, int D, int L_cap, float scale, void* workspace,
+                            const int32_t* gamma, void* out, bool out_bf16, int B, int gamma_max, int Hq,
+                            int Hkv, int D, int L_cap, int window, int sinks, float scale, void* workspace,
                             const AttentionPlan& plan, int32_t* status, hipStream_t stream);
+int attention_kv4_plan(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap, int window, int sinks,
+                       AttentionPlan* plan);
+int launch_attention_kv4(const void* q, const void* k_codes, const void* k_powers, const void* v_codes,
+                         const void* v_powers, const uint8_t* cache_mask, const int32_t* kv_len, const int32_t* gamma,
+                         void* out, bool out_bf16, int B, int gamma_max, int Hq, int Hkv, int D, int L_cap, int window,
+                         int sinks, float scale, void* workspace, const AttentionPlan& plan, int32_t* status,
+                         hipStream_t stream);
+// The dispatch order of (sequence, kv head, query chunk, split) jobs, longest first.
+int launch_attention_order(const int32_t* kv_len, const int32_t* gamma, int B, int gamma_max, int Hkv, int q_chunks,
+                           int L_cap, int window, int sinks, int tile, int split_keys, int n_splits, int32_t* order,
+                           hipStream_t stream);
 
 struct AcceptPlan {
   int chunk;          // vocabulary entries per workgroup task

@@ -68,3 +68,29 @@ def test_kv4_append(lib):
     cases += [(1, 120, EINVAL), (3, 132, EINVAL), (14, 0, EINVAL), (14, 65536, EINVAL), (15, -1, EINVAL),
               (15, 100, EINVAL), (16, 0, EINVAL), (17, 32, EUNSUPPORTED), (18, 0, EINVAL), (18, (1 << 22) + 1, EINVAL)]
     _refusals(lib.specrouter_kv4_append, good, cases)
+
+
+@no_device
+def test_window_attention(lib):
+    # q, k, v, mask, kv_len, gamma, out, dtype, B, gmax, Hq, Hkv, D, L_cap, window, sinks, scale, ws, bytes, status, stream
+    good = [P, P, P, None, P, P, P, 1, 2, 4, 8, 2, 128, 512, 64, 4, 0.1, None, 0, None, None]
+    cases = [(i, None, EINVAL) for i in (0, 1, 2, 4, 5, 6)] + [(i, ODD, EINVAL) for i in (0, 1, 2, 6)]
+    cases += [(7, 2, EUNSUPPORTED), (8, 0, EINVAL), (9, 17, EINVAL), (9, -1, EINVAL), (11, 3, EINVAL),
+              (12, 96, EUNSUPPORTED), (13, 4, EINVAL), (13, (1 << 22) + 1, EINVAL), (14, 0, EINVAL), (14, -5, EINVAL),
+              (15, -1, EINVAL)]
+    cases += [(16, s, EINVAL) for s in (0.0, -0.1, float("nan"), float("inf"))]
+    _refusals(lib.specrouter_verify_attention_window, good, cases)
+    assert lib.specrouter_verify_attention_window_workspace_size(2, 4, 8, 2, 128, 512, 0, 4) == 0
+
+
+@no_device
+def test_kv4_attention(lib):
+    # q, kc, kp, vc, vp, mask, kv_len, gamma, out, dtype, B, gmax, Hq, Hkv, D, L_cap, window, sinks, scale, ws, bytes, ...
+    good = [P, P, P, P, P, None, P, P, P, 0, 2, 4, 8, 2, 64, 512, 0, 0, 0.1, None, 0, None, None]
+    cases = [(i, None, EINVAL) for i in (0, 1, 2, 3, 4, 6, 7, 8)] + [(i, ODD, EINVAL) for i in (0, 1, 3, 8)]
+    cases += [(i, ctypes.c_void_p(4098), EINVAL) for i in (2, 4)]
+    cases += [(9, 5, EUNSUPPORTED), (10, 65536, EINVAL), (11, 17, EINVAL), (12, 9, EINVAL), (14, 32, EUNSUPPORTED),
+              (15, 4, EINVAL), (16, -1, EINVAL), (17, -1, EINVAL)]
+    cases += [(18, s, EINVAL) for s in (0.0, float("nan"), float("inf"))]
+    _refusals(lib.specrouter_verify_attention_kv4, good, cases)
+    assert lib.specrouter_verify_attention_kv4_workspace_size(2, 4, 8, 3, 64, 512, 0, 0) == 0
