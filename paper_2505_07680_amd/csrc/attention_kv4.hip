@@ -26,6 +26,8 @@
 //   * softmax as over bf16: a row's reference is raised only when a tile exceeds
 //     it by more than 2^8, P rounds to bf16.
 
+#include <type_traits>
+
 #include "attention_common.h"
 
 namespace sr {
@@ -36,12 +38,15 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr int kTile = 32;   // keys per tile of a wave
 constexpr int kRing4 = 2;   // tiles in flight per wave
 constexpr int kMaxNQ4 = 3;  // 16-row query blocks per wave: more than 48 rows go to further query chunks
+constexpr int kRegNQ = 2;   // of them with their query rows in registers
 
 template <int D, int NQ>
 struct Lds4 {
   static constexpr int kRow = D * 2;               // bytes of a widened V row
   static constexpr int kSlot = kTile * kRow;       // per wave
-  static constexpr int kStage = kWaves * kSlot;
+  static constexpr int kQRows = NQ > kRegNQ ? 16 * (NQ - kRegNQ) : 0;  // query rows that stay here
+  static constexpr int kQ = kWaves * kSlot;
+  static constexpr int kStage = kQ + kQRows * D * 2;
   static constexpr int kComb = MergeLds<D, NQ, 1>::kComb;
   static constexpr int kBytes = kStage > kComb ? kStage : kComb;
 };
@@ -54,6 +59,10 @@ __device__ __forceinline__ u32x4 widen(uint32_t codes, float scale) {
   v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
   v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
   return v;
+}
+
+__device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{lo, hi}, bf16x2));
 }
 
 // Where 16-byte chunk c of V row r sits in its row.
@@ -151,7 +160,7 @@ attn_kv4_kernel(Kv4Args a) {
   const __amdgpu_buffer_rsrc_t rkp = make_rsrc(a.kp + slab * (D / 32), (size_t)a.L_cap * (D / 32));
   const __amdgpu_buffer_rsrc_t rvp = make_rsrc(a.vp + slab * (D / 32), (size_t)a.L_cap * (D / 32));
   const uint8_t* mrow = a.mask ? a.mask + (size_t)b * a.L_cap : nullptr;
-  const uint8_t* mload = mrow ? mrow : a.kc + slab * (D / 2);
+  const __amdgpu_buffer_rsrc_t rm = make_rsrc(mrow ? mrow : a.kc, mrow ? (size_t)L : 0);  // (no mask: no traffic)
 
   floatx4 o[DB][NQ];
   float m_run[NQ], l_run[NQ];
@@ -168,31 +177,41 @@ attn_kv4_kernel(Kv4Args a) {
   const int t_end = min(reach.tiles, t0 + tiles_per);
   auto tile_key = [&](int t) __attribute__((always_inline)) { return t < t_end ? reach.start(t) : L; };
   constexpr int kPolicy = NT ? kStreamLoad : 0;
+  // Every fetch issues the same loads; lanes past the length, and all lanes past
+  // the stream's last tile, read out of range (as zero, with no traffic).
+  const uint32_t lane_off = (uint32_t)(l16 * (D / 2) + lg * (EL / 2));
+  const uint32_t lane_poff = (uint32_t)(l16 * (D / 32) + lg * EL / 32);
   auto fetch = [&](int t, Stage4<D>& st) __attribute__((always_inline)) {
     const int kb0 = tile_key(t);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int row = kb0 + u * 16 + l16;
-      const uint32_t off = row < L ? (uint32_t)row * (D / 2) + (uint32_t)lg * (EL / 2) : kOutOfRange;
-      const uint32_t poff = row < L ? (uint32_t)row * (D / 32) + (uint32_t)(lg * EL / 32) : kOutOfRange;
+      const int row0u = kb0 + u * 16;
+      const bool in = l16 < L - row0u;
+      const uint32_t off = in ? lane_off : kOutOfRange, poff = in ? lane_poff : kOutOfRange;
+      const int at = row0u * (D / 2), pat = row0u * (D / 32);
       if constexpr (D == 128) {
-        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rkc, off, 0, kPolicy));
-        const u32x4 y = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rvc, off, 0, kPolicy));
+        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rkc, off, at, kPolicy));
+        const u32x4 y = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rvc, off, at, kPolicy));
 #pragma unroll
         for (int e = 0; e < 4; ++e) st.k[u][e] = x[e], st.v[u][e] = y[e];
       } else {
-        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rkc, off, 0, kPolicy));
-        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rvc, off, 0, kPolicy));
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rkc, off, at, kPolicy));
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rvc, off, at, kPolicy));
         st.k[u][0] = x[0], st.k[u][1] = x[1], st.v[u][0] = y[0], st.v[u][1] = y[1];
       }
-      st.kp[u] = __builtin_amdgcn_raw_buffer_load_b8(rkp, poff, 0, kPolicy);
-      st.vp[u] = __builtin_amdgcn_raw_buffer_load_b8(rvp, poff, 0, kPolicy);
+      st.kp[u] = __builtin_amdgcn_raw_buffer_load_b8(rkp, poff, pat, kPolicy);
+      st.vp[u] = __builtin_amdgcn_raw_buffer_load_b8(rvp, poff, pat, kPolicy);
     }
-    st.mbyte = mload[min(kb0 + (lane & (kTile - 1)), L - 1)];
+    st.mbyte = __builtin_amdgcn_raw_buffer_load_b8(rm, lane & (kTile - 1), kb0, 0);
   };
+  // Bits 0 .. n - 1
+  auto low_bits = [](int n) __attribute__((always_inline)) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; };
 
   // This lane's part of the query rows: qf[qg][ks] holds Q[qg 16 + l16][lg EL + 8 ks ..].
-  bf16x8 qf[NQ][KS];
+  // (A third block's would not fit the registers beside its accumulators: its
+  // rows are read from LDS, in the lanes' order, for every tile.)
+  constexpr int kReg = NQ < kRegNQ ? NQ : kRegNQ;
+  bf16x8 qf[kReg][KS];
 #pragma unroll
   for (int qg = 0; qg < NQ; ++qg) {
     const int r = row0 + qg * 16 + l16;
@@ -200,41 +219,66 @@ attn_kv4_kernel(Kv4Args a) {
     const uint16_t* src = a.q + ((size_t)(b * (a.gmax + 1) + i) * a.Hq + hh) * D + lg * EL;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      const u32x4 x = *(const u32x4*)(src + ks * 8);
-      qf[qg][ks] = __builtin_bit_cast(bf16x8, r < Mb ? x : u32x4{0u, 0u, 0u, 0u});
+      const u32x4 y = *(const u32x4*)(src + ks * 8);
+      const u32x4 x = r < Mb ? y : u32x4{0u, 0u, 0u, 0u};
+      if (qg < kReg) qf[qg < kReg ? qg : 0][ks] = __builtin_bit_cast(bf16x8, x);
+      else if (ws == 0) *(u32x4*)(lds + LL::kQ + (((qg - kReg) * KS + ks) * 64 + lane) * 16) = x;
     }
   }
-  unsigned char* slot = lds + ws * LL::kSlot;
+  if (NQ > kReg) __syncthreads();
+  auto query = [&](int qg, int ks) __attribute__((always_inline)) {
+    return qg < kReg ? qf[qg < kReg ? qg : 0][ks]
+                     : *(const bf16x8*)(lds + LL::kQ + (((qg - kReg) * KS + ks) * 64 + lane) * 16);
+  };
+  // This lane's V offsets in LDS: its row's first chunk as written, and the run it
+  // names as read (the tile's other half is 16 rows on). The permutation turns the
+  // low three bits of a chunk's number, so its other chunks lie at these offsets
+  // with bits turned too, and columns 64 apart 128 bytes apart.
+  const int v_write = ws * LL::kSlot + l16 * LL::kRow + chunk_at(lg * KS, l16) * 16;
+  const int v_row = lg * 4 + (l16 >> 2);
+  const int v_read = ws * LL::kSlot + v_row * LL::kRow + chunk_at((l16 & 3) >> 1, v_row) * 16 + (l16 & 1) * 8;
 
-  auto step = [&](int& t, Stage4<D>& st) __attribute__((always_inline)) {
+  // One tile for the first NL of the wave's row blocks (the others hold no live row).
+  auto step = [&](auto blocks, int& t, Stage4<D>& st) __attribute__((always_inline)) {
+    constexpr int NL = decltype(blocks)::value;
     const int kb0 = tile_key(t);
-    const int key = kb0 + (lane & (kTile - 1));
-    const bool key_ok = lane < kTile && key < L && (key >= reach.first_key || key < sinks) &&
-                        (mrow == nullptr || st.mbyte != 0u);
-    const uint32_t vbits = (uint32_t)__ballot(key_ok);  // keys that some row may see
-    // ---- V to LDS
+    // keys that some row may see: below the length, in reach, valid
+    uint32_t vbits = low_bits(L - kb0) & (~low_bits(reach.first_key - kb0) | low_bits(sinks - kb0));
+    if (mrow) vbits &= (uint32_t)__ballot(st.mbyte != 0u);
+    // ---- V to LDS (rows that no row sees as zeros, whatever they hold)
+    if (vbits != ~0u) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bool seen = (vbits >> (u * 16 + l16)) & 1u;
+        st.vp[u] = seen ? st.vp[u] : 0u;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) st.v[u][ks] = seen ? st.v[u][ks] : 0u;
+      }
+    }
+    // (the offset and the lane's numbers below are hidden from the optimiser, which
+    // would keep all that follows from them in registers across the loop)
+    int vw = v_write;
+    asm volatile("" : "+v"(vw));
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const bool seen = (vbits >> (u * 16 + l16)) & 1u;
-      const float scale = __uint_as_float(seen ? st.vp[u] << 23 : 0u);
-      const int r = u * 16 + l16;
+      const float scale = __uint_as_float(st.vp[u] << 23);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        *(u32x4*)(slot + r * LL::kRow + chunk_at(lg * KS + ks, r) * 16) = widen(seen ? st.v[u][ks] : 0u, scale);
+        *(u32x4*)(lds + (vw ^ (ks * 16)) + u * 16 * LL::kRow) = widen(st.v[u][ks], scale);
     }
     // ---- S^T = K Q^T
-    floatx4 sacc[2][NQ];
+    floatx4 sacc[2][NL];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const float scale = __uint_as_float(st.kp[u] << 23);
 #pragma unroll
-      for (int qg = 0; qg < NQ; ++qg) sacc[u][qg] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int qg = 0; qg < NL; ++qg) sacc[u][qg] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const bf16x8 ka = __builtin_bit_cast(bf16x8, widen(st.k[u][ks], scale));
 #pragma unroll
-        for (int qg = 0; qg < NQ; ++qg)
-          sacc[u][qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[qg][ks], sacc[u][qg], 0, 0, 0);
+        for (int qg = 0; qg < NL; ++qg)
+          sacc[u][qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, query(qg, ks), sacc[u][qg], 0, 0, 0);
       }
     }
     wave_lds_sync();
@@ -242,70 +286,65 @@ attn_kv4_kernel(Kv4Args a) {
     __builtin_amdgcn_sched_barrier(0);
     fetch(t, st);
     __builtin_amdgcn_sched_barrier(0);
-    // ---- mask, online softmax, P in bf16 (lane: keys u 16 + lg 4 + e of query l16)
-    const bool full = vbits == 0xffffffffu && kb0 + kTile - 1 <= causal0 &&
-                      (kb0 > L - 1 - window || kb0 + kTile <= sinks);  // wave-uniform
-    bf16x8 pb[NQ];
+    // ---- online softmax, P in bf16 (lane: keys u 16 + lg 4 + e of query l16)
+    if (!(vbits == 0xffffffffu && kb0 + kTile - 1 <= causal0 && (kb0 > L - 1 - window || kb0 + kTile <= sinks))) {
+      // (wave-uniform: not every row sees the whole tile)
+      int r16 = l16, r4 = lg * 4;
+      asm volatile("" : "+v"(r16), "+v"(r4));
 #pragma unroll
-    for (int qg = 0; qg < NQ; ++qg) {
-      pb[qg] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-      if (row0 + qg * 16 < Mb) {
-        const int r = row0 + qg * 16 + l16;
-        float s[8];
-        float mt = kNegInf;
-        if (full) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            s[e] = sacc[e / 4][qg][e % 4];
-            mt = fmaxf(mt, s[e]);
-          }
-          mt *= a.scale_log2;
-        } else {
-          const int lim = r < Mb ? causal0 + r / G : -1;  // last key this query row sees
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int kl = (e / 4) * 16 + lg * 4 + e % 4;
-            const int k = kb0 + kl;
-            const bool vis = ((vbits >> kl) & 1u) && k <= lim && (k > lim - window || k < sinks);
-            s[e] = vis ? sacc[e / 4][qg][e % 4] * a.scale_log2 : kNegInf;
-            mt = fmaxf(mt, s[e]);
-          }
-        }
-        mt = max_across_rows(mt);
-        const bool grow = mt > m_run[qg] + kLazy;
-        const float mref = grow ? mt : m_run[qg];
-        const float alpha = m_run[qg] == mref ? 1.f : exp2_hw(m_run[qg] - mref);
-        const float mr = mref == kNegInf ? 0.f : mref;  // (-inf: no key of the row so far)
-        float pk[8];
-        float ls = 0.f;
+      for (int qg = 0; qg < NL; ++qg) {
+        const int r = row0 + qg * 16 + r16;
+        const int lim = r < Mb ? causal0 + r / G : -1;  // last key this query row sees
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          pk[e] = exp2_hw(full ? fmaf(s[e], a.scale_log2, -mr) : s[e] - mr);
-          ls += pk[e];
+          const int kl = (e / 4) * 16 + r4 + e % 4;
+          const int k = kb0 + kl;
+          const bool vis = (((vbits >> kl) & 1u) != 0u) & (k <= lim) & ((k > lim - window) | (k < sinks));
+          sacc[e / 4][qg][e % 4] = vis ? sacc[e / 4][qg][e % 4] : kNegInf;
         }
-        ls = sum_across_rows(ls);
-        l_run[qg] = l_run[qg] * alpha + ls;
-        m_run[qg] = mref;
-        if (__ballot(grow) != 0ull) {
-#pragma unroll
-          for (int db = 0; db < DB; ++db) o[db][qg] *= alpha;
-        }
-        pb[qg] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(pk[0], pk[1]), pack_bf16x2(pk[2], pk[3]),
-                                                  pack_bf16x2(pk[4], pk[5]), pack_bf16x2(pk[6], pk[7])});
       }
+    }
+    bf16x8 pb[NL];
+#pragma unroll
+    for (int qg = 0; qg < NL; ++qg) {
+      float mt = kNegInf;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mt = fmaxf(mt, sacc[e / 4][qg][e % 4]);
+      mt *= a.scale_log2;
+      // The reference stands until a score exceeds it by more than 2^kLazy: only
+      // then do the row's four lanes need their common maximum.
+      if (__ballot(mt > m_run[qg] + kLazy) != 0ull) {
+        mt = max_across_rows(mt);
+        const float mref = mt > m_run[qg] + kLazy ? mt : m_run[qg];
+        const float alpha = m_run[qg] == mref ? 1.f : exp2_hw(m_run[qg] - mref);
+        m_run[qg] = mref;
+        l_run[qg] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db][qg] *= alpha;
+      }
+      const float mr = m_run[qg] == kNegInf ? 0.f : m_run[qg];  // (-inf: no key of the row so far)
+      float pk[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        pk[e] = exp2_hw(fmaf(sacc[e / 4][qg][e % 4], a.scale_log2, -mr));
+        l_run[qg] += pk[e];  // (of this lane's keys; the row's four lanes are summed at the end)
+      }
+      pb[qg] = __builtin_bit_cast(bf16x8, u32x4{to_bf16x2(pk[0], pk[1]), to_bf16x2(pk[2], pk[3]),
+                                                to_bf16x2(pk[4], pk[5]), to_bf16x2(pk[6], pk[7])});
     }
     // ---- O^T += V^T P^T over the 32 keys: contraction slot lg 8 + e is key
     // lg 4 + e (e < 4) or 16 + lg 4 + e - 4, as the scores lie in the registers
-    const int vr = lg * 4 + (l16 >> 2);
+    int vr = v_read;
+    asm volatile("" : "+v"(vr));
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-      const unsigned char* p0 = slot + vr * LL::kRow + chunk_at(db * 2 + ((l16 & 3) >> 1), vr) * 16 + (l16 & 1) * 8;
+      const unsigned char* p0 = lds + (vr ^ (db % 4 * 32)) + db / 4 * 128;
       const shortx4 va0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p0);
       const shortx4 va1 =
           __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(p0 + 16 * LL::kRow));
       const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(va0, va1, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-      for (int qg = 0; qg < NQ; ++qg)
+      for (int qg = 0; qg < NL; ++qg)
         o[db][qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[qg], o[db][qg], 0, 0, 0);
     }
     wave_lds_sync();  // this tile's LDS reads are issued before the slot is rewritten
@@ -321,10 +360,18 @@ attn_kv4_kernel(Kv4Args a) {
     __builtin_amdgcn_sched_barrier(0);
   }
   // (a step past the stream's last tile reads nothing and adds nothing)
-  while (tr[0] < t_end) {
+  auto loop = [&](auto blocks) __attribute__((always_inline)) {
+    while (tr[0] < t_end) {
 #pragma unroll
-    for (int r = 0; r < kRing4; ++r) step(tr[r], ring[r]);
-  }
+      for (int r = 0; r < kRing4; ++r) step(blocks, tr[r], ring[r]);
+    }
+  };
+  const int live = min(NQ, (Mb - row0 + 15) / 16);
+  if (NQ >= 3 && live >= 3) loop(std::integral_constant<int, NQ >= 3 ? 3 : 1>{});
+  else if (NQ >= 2 && live >= 2) loop(std::integral_constant<int, NQ >= 2 ? 2 : 1>{});
+  else loop(std::integral_constant<int, 1>{});
+#pragma unroll
+  for (int qg = 0; qg < NQ; ++qg) l_run[qg] = sum_across_rows(l_run[qg]);
   __syncthreads();
 
   const JobRows J{row0, row_end, Mb, R, split, ns, a.n_splits, job, P, (size_t)(b * a.Hkv + g)};
