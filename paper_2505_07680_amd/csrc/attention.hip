@@ -551,7 +551,7 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
   __syncthreads();
 
   const JobRows J{row0, row_end, Mb, R, split, ns, n_splits, job, P, (size_t)(b * Hkv + g)};
-  merge_and_store<D, NQ, QG, Lds<D, NQ, QG>::kBytes, WIN>(
+  merge_and_store<MergeLds<D, NQ, QG>, D, NQ, QG, Lds<D, NQ, QG>::kBytes, WIN>(
       lds, o, m_run, l_run, J, part_o, part_ml, counters, store);
 }
 

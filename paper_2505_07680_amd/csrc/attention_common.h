@@ -38,12 +38,14 @@ struct Shape {
 };
 
 // LDS of the merge of the four stream states of each query group: the columns
-// are reduced in kPasses passes so that a group's four fp32 slices fit in 72 KB
-// (two four-wave workgroups per CU, or one of eight, fit in its 160 KB).
-template <int D, int NQ, int QG>
+// are reduced in kPasses passes so that a group's four fp32 slices fit in kMost
+// bytes (72 KB: two four-wave workgroups per CU, or one of eight, fit in its 160
+// KB).
+constexpr int kMergeMost = 73728;
+template <int D, int NQ, int QG, int kMost = kMergeMost>
 struct MergeLds {
   static constexpr int MQ = 16 * NQ;
-  static constexpr int kPasses = (kWaves * MQ * D * 4 <= 73728) ? 1 : (kWaves * MQ * D * 2 <= 73728) ? 2 : 4;
+  static constexpr int kPasses = (kWaves * MQ * D * 4 <= kMost) ? 1 : (kWaves * MQ * D * 2 <= kMost) ? 2 : 4;
   static constexpr int kDp = D / kPasses;                 // columns per pass
   static constexpr int kRowStride = kDp + 4;              // floats; padded against bank conflicts
   static constexpr int kSlot = MQ * kRowStride;           // floats per wave slice
@@ -118,7 +120,7 @@ struct JobRows {
 // for its group's rows; store(r, col, x) writes four columns of an output row.
 // A row whose sum is 0 (no visible key) is 0; so is one whose sum is NaN unless
 // NANS, where that row is NaN (the call without a window keeps what it did).
-template <int D, int NQ, int QG, int kLdsBytes, bool NANS, class Store>
+template <class LL, int D, int NQ, int QG, int kLdsBytes, bool NANS, class Store>
 __device__ __forceinline__ void merge_and_store(unsigned char* lds, const floatx4 (&o)[D / 16][NQ],
                                                 const float (&m_run)[NQ], const float (&l_run)[NQ],
                                                 const JobRows& J, float* part_o, float* part_ml,
@@ -139,7 +141,6 @@ __device__ __forceinline__ void merge_and_store(unsigned char* lds, const floatx
   const int lg = lane >> 4;
 
   // ---- merge the four stream states of each query group (every wave and lane takes part)
-  using LL = MergeLds<D, NQ, QG>;
   const int tg = tid - h * 64 * kWaves;                               // thread index in the group
   float* slots = (float*)lds + h * kWaves * LL::kSlot;                  // [kWaves][MQ][kRowStride]
   float* mlx = (float*)(lds + LL::kMl) + h * (kWaves + 1) * 2 * MQ;     // [kWaves][2][MQ]: each stream's (m, l)

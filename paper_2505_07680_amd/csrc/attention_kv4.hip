@@ -36,18 +36,20 @@ namespace {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = 32;   // keys per tile of a wave
-constexpr int kRing4 = 2;   // tiles in flight per wave
 constexpr int kMaxNQ4 = 3;  // 16-row query blocks per wave: more than 48 rows go to further query chunks
+constexpr int kMergeMost4 = 49152;  // the merge's LDS: three workgroups fit a CU's
 constexpr int kRegNQ = 2;   // of them with their query rows in registers
 
 template <int D, int NQ>
 struct Lds4 {
   static constexpr int kRow = D * 2;               // bytes of a widened V row
-  static constexpr int kSlot = kTile * kRow;       // per wave
-  static constexpr int kQRows = NQ > kRegNQ ? 16 * (NQ - kRegNQ) : 0;  // query rows that stay here
+  static constexpr int kSlot = kTile * kRow;       // a tile's V, per wave
+  static constexpr int kReg = NQ < 3 ? NQ : kRegNQ;
+  static constexpr int kQRows = 16 * (NQ - kReg);  // query rows that stay here
   static constexpr int kQ = kWaves * kSlot;
   static constexpr int kStage = kQ + kQRows * D * 2;
-  static constexpr int kComb = MergeLds<D, NQ, 1>::kComb;
+  using Merge = MergeLds<D, NQ, 1, kMergeMost4>;
+  static constexpr int kComb = Merge::kComb;
   static constexpr int kBytes = kStage > kComb ? kStage : kComb;
 };
 
@@ -65,14 +67,19 @@ __device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{lo, hi}, bf16x2));
 }
 
+// A branch that is seldom taken: its code goes out of the way (a taken branch
+// costs a wave about 45 cycles).
+__device__ __forceinline__ bool rare(bool x) { return __builtin_expect(x, 0); }
+
 // Where 16-byte chunk c of V row r sits in its row.
 __device__ __forceinline__ int chunk_at(int c, int r) { return c ^ (((r & 3) << 1) | ((r >> 2) & 1)); }
 
 template <int D>
 struct Stage4 {  // a 32-key tile in flight: rows u 16 + l16
   uint32_t k[2][D / 32], v[2][D / 32];
-  uint32_t kp[2], vp[2];
-  uint32_t mbyte;  // validity byte of key (lane mod 32)
+  uint8_t kp[2], vp[2];
+  uint8_t mbyte;
+  int key;         // first key
 };
 
 struct Kv4Args {
@@ -91,8 +98,11 @@ struct Kv4Args {
   int32_t* status;
 };
 
-template <int D, int NQ, bool NT>
-__global__ void __launch_bounds__(64 * kWaves, NQ == 1 ? 3 : 2)
+// RING: tiles in flight per wave (see attention_kv4_plan). With one and two row
+// blocks, 168 registers, three waves fit a SIMD; what is kept in scratch there is the
+// merge's.
+template <int D, int NQ, int RING, bool NT>
+__global__ void __launch_bounds__(64 * kWaves, NQ == 1 || (NQ == 2 && RING == 1) ? 3 : 2)
 attn_kv4_kernel(Kv4Args a) {
   constexpr int MQ = 16 * NQ;
   constexpr int DB = D / 16;
@@ -183,6 +193,7 @@ attn_kv4_kernel(Kv4Args a) {
   const uint32_t lane_poff = (uint32_t)(l16 * (D / 32) + lg * EL / 32);
   auto fetch = [&](int t, Stage4<D>& st) __attribute__((always_inline)) {
     const int kb0 = tile_key(t);
+    st.key = kb0;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int row0u = kb0 + u * 16;
@@ -204,13 +215,15 @@ attn_kv4_kernel(Kv4Args a) {
     }
     st.mbyte = __builtin_amdgcn_raw_buffer_load_b8(rm, lane & (kTile - 1), kb0, 0);
   };
+  // Tiles from key inner_lo to inner_hi are seen whole by every row (but for the mask).
+  const int inner_lo = L - window, inner_hi = causal0 + 1 - kTile;
   // Bits 0 .. n - 1
   auto low_bits = [](int n) __attribute__((always_inline)) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; };
 
   // This lane's part of the query rows: qf[qg][ks] holds Q[qg 16 + l16][lg EL + 8 ks ..].
   // (A third block's would not fit the registers beside its accumulators: its
   // rows are read from LDS, in the lanes' order, for every tile.)
-  constexpr int kReg = NQ < kRegNQ ? NQ : kRegNQ;
+  constexpr int kReg = LL::kReg;
   bf16x8 qf[kReg][KS];
 #pragma unroll
   for (int qg = 0; qg < NQ; ++qg) {
@@ -241,54 +254,58 @@ attn_kv4_kernel(Kv4Args a) {
   // One tile for the first NL of the wave's row blocks (the others hold no live row).
   auto step = [&](auto blocks, int& t, Stage4<D>& st) __attribute__((always_inline)) {
     constexpr int NL = decltype(blocks)::value;
-    const int kb0 = tile_key(t);
+    const int kb0 = st.key;
     // keys that some row may see: below the length, in reach, valid
-    uint32_t vbits = low_bits(L - kb0) & (~low_bits(reach.first_key - kb0) | low_bits(sinks - kb0));
+    const bool inner = kb0 >= inner_lo && kb0 <= inner_hi;
+    uint32_t vbits = ~0u;
+    if (rare(!inner)) vbits = low_bits(L - kb0) & (~low_bits(reach.first_key - kb0) | low_bits(sinks - kb0));
     if (mrow) vbits &= (uint32_t)__ballot(st.mbyte != 0u);
-    // ---- V to LDS (rows that no row sees as zeros, whatever they hold)
-    if (vbits != ~0u) {
+    if (rare(vbits != ~0u)) {  // V rows that no row sees are zeros, whatever they hold
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const bool seen = (vbits >> (u * 16 + l16)) & 1u;
-        st.vp[u] = seen ? st.vp[u] : 0u;
+        st.vp[u] = seen ? st.vp[u] : (uint8_t)0;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) st.v[u][ks] = seen ? st.v[u][ks] : 0u;
       }
     }
-    // (the offset and the lane's numbers below are hidden from the optimiser, which
+    // ---- S^T = K Q^T
+    floatx4 sacc[2][NL];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int qg = 0; qg < NL; ++qg) sacc[u][qg] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 ka[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        ka[u] = __builtin_bit_cast(bf16x8, widen(st.k[u][ks], __uint_as_float((uint32_t)st.kp[u] << 23)));
+#pragma unroll
+      for (int qg = 0; qg < NL; ++qg)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          sacc[u][qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[u], query(qg, ks), sacc[u][qg], 0, 0, 0);
+    }
+    // ---- V to LDS, while the products finish
+    // (the offsets and the lane's numbers below are hidden from the optimiser, which
     // would keep all that follows from them in registers across the loop)
     int vw = v_write;
     asm volatile("" : "+v"(vw));
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const float scale = __uint_as_float(st.vp[u] << 23);
+      const float scale = __uint_as_float((uint32_t)st.vp[u] << 23);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
         *(u32x4*)(lds + (vw ^ (ks * 16)) + u * 16 * LL::kRow) = widen(st.v[u][ks], scale);
     }
-    // ---- S^T = K Q^T
-    floatx4 sacc[2][NL];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float scale = __uint_as_float(st.kp[u] << 23);
-#pragma unroll
-      for (int qg = 0; qg < NL; ++qg) sacc[u][qg] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 ka = __builtin_bit_cast(bf16x8, widen(st.k[u][ks], scale));
-#pragma unroll
-        for (int qg = 0; qg < NL; ++qg)
-          sacc[u][qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, query(qg, ks), sacc[u][qg], 0, 0, 0);
-      }
-    }
     wave_lds_sync();
-    t += kRing4 * kWaves;
+    t += RING * kWaves;
     __builtin_amdgcn_sched_barrier(0);
     fetch(t, st);
     __builtin_amdgcn_sched_barrier(0);
     // ---- online softmax, P in bf16 (lane: keys u 16 + lg 4 + e of query l16)
-    if (!(vbits == 0xffffffffu && kb0 + kTile - 1 <= causal0 && (kb0 > L - 1 - window || kb0 + kTile <= sinks))) {
-      // (wave-uniform: not every row sees the whole tile)
+    if (rare(!inner || vbits != ~0u)) {  // (wave-uniform: not every row sees the whole tile)
       int r16 = l16, r4 = lg * 4;
       asm volatile("" : "+v"(r16), "+v"(r4));
 #pragma unroll
@@ -304,24 +321,33 @@ attn_kv4_kernel(Kv4Args a) {
         }
       }
     }
+    // A row's reference stands until a score exceeds it by more than 2^kLazy: only
+    // then do its four lanes need their common maximum.
     bf16x8 pb[NL];
+    float mt[NL];
+    bool over = false;
 #pragma unroll
     for (int qg = 0; qg < NL; ++qg) {
-      float mt = kNegInf;
+      mt[qg] = kNegInf;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mt = fmaxf(mt, sacc[e / 4][qg][e % 4]);
-      mt *= a.scale_log2;
-      // The reference stands until a score exceeds it by more than 2^kLazy: only
-      // then do the row's four lanes need their common maximum.
-      if (__ballot(mt > m_run[qg] + kLazy) != 0ull) {
-        mt = max_across_rows(mt);
-        const float mref = mt > m_run[qg] + kLazy ? mt : m_run[qg];
+      for (int e = 0; e < 8; ++e) mt[qg] = fmaxf(mt[qg], sacc[e / 4][qg][e % 4]);
+      mt[qg] *= a.scale_log2;
+      over |= mt[qg] > m_run[qg] + kLazy;
+    }
+    if (rare(__ballot(over) != 0ull)) {
+#pragma unroll
+      for (int qg = 0; qg < NL; ++qg) {
+        const float m = max_across_rows(mt[qg]);
+        const float mref = m > m_run[qg] + kLazy ? m : m_run[qg];
         const float alpha = m_run[qg] == mref ? 1.f : exp2_hw(m_run[qg] - mref);
         m_run[qg] = mref;
         l_run[qg] *= alpha;
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[db][qg] *= alpha;
       }
+    }
+#pragma unroll
+    for (int qg = 0; qg < NL; ++qg) {
       const float mr = m_run[qg] == kNegInf ? 0.f : m_run[qg];  // (-inf: no key of the row so far)
       float pk[8];
 #pragma unroll
@@ -333,28 +359,37 @@ attn_kv4_kernel(Kv4Args a) {
                                                 to_bf16x2(pk[4], pk[5]), to_bf16x2(pk[6], pk[7])});
     }
     // ---- O^T += V^T P^T over the 32 keys: contraction slot lg 8 + e is key
-    // lg 4 + e (e < 4) or 16 + lg 4 + e - 4, as the scores lie in the registers
+    // lg 4 + e (e < 4) or 16 + lg 4 + e - 4, as the scores lie in the registers. Two
+    // column blocks' reads are in flight before a block's products.
     int vr = v_read;
     asm volatile("" : "+v"(vr));
+    shortx4 va[3][2];
+    auto read = [&](int db) __attribute__((always_inline)) {
+      const unsigned char* p0 = lds + (vr ^ (db % 4 * 32)) + db / 4 * 128;
+      va[db % 3][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p0);
+      va[db % 3][1] =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(p0 + 16 * LL::kRow));
+    };
+    read(0);
+    read(1);
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-      const unsigned char* p0 = lds + (vr ^ (db % 4 * 32)) + db / 4 * 128;
-      const shortx4 va0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p0);
-      const shortx4 va1 =
-          __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(p0 + 16 * LL::kRow));
-      const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(va0, va1, 0, 1, 2, 3, 4, 5, 6, 7));
+      if (db + 2 < DB) read(db + 2);
+      const bf16x8 v =
+          __builtin_bit_cast(bf16x8, __builtin_shufflevector(va[db % 3][0], va[db % 3][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
       for (int qg = 0; qg < NL; ++qg)
-        o[db][qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[qg], o[db][qg], 0, 0, 0);
+        o[db][qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pb[qg], o[db][qg], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
     wave_lds_sync();  // this tile's LDS reads are issued before the slot is rewritten
   };
 
   __builtin_amdgcn_sched_barrier(0);
-  Stage4<D> ring[kRing4];
-  int tr[kRing4];
+  Stage4<D> ring[RING];
+  int tr[RING];
 #pragma unroll
-  for (int r = 0; r < kRing4; ++r) {
+  for (int r = 0; r < RING; ++r) {
     tr[r] = t0 + ws + r * kWaves;
     fetch(tr[r], ring[r]);
     __builtin_amdgcn_sched_barrier(0);
@@ -363,7 +398,7 @@ attn_kv4_kernel(Kv4Args a) {
   auto loop = [&](auto blocks) __attribute__((always_inline)) {
     while (tr[0] < t_end) {
 #pragma unroll
-      for (int r = 0; r < kRing4; ++r) step(blocks, tr[r], ring[r]);
+      for (int r = 0; r < RING; ++r) step(blocks, tr[r], ring[r]);
     }
   };
   const int live = min(NQ, (Mb - row0 + 15) / 16);
@@ -375,21 +410,21 @@ attn_kv4_kernel(Kv4Args a) {
   __syncthreads();
 
   const JobRows J{row0, row_end, Mb, R, split, ns, a.n_splits, job, P, (size_t)(b * a.Hkv + g)};
-  merge_and_store<D, NQ, 1, LL::kBytes, true>(lds, o, m_run, l_run, J, a.part_o, a.part_ml, a.counters, store);
+  merge_and_store<typename LL::Merge, D, NQ, 1, LL::kBytes, true>(lds, o, m_run, l_run, J, a.part_o, a.part_ml, a.counters, store);
 }
 
 typedef void (*Kv4Kernel)(Kv4Args);
 
+// (more than one query chunk takes at least two row blocks)
 template <int D>
-Kv4Kernel pick_kv4(int nq, bool nt) {
-  switch (nq) {
-    case 1: return nt ? attn_kv4_kernel<D, 1, true> : attn_kv4_kernel<D, 1, false>;
-    case 2: return nt ? attn_kv4_kernel<D, 2, true> : attn_kv4_kernel<D, 2, false>;
-    default: return nt ? attn_kv4_kernel<D, 3, true> : attn_kv4_kernel<D, 3, false>;
-  }
+Kv4Kernel pick_kv4(int nq, int ring, bool nt) {
+  if (nq == 1) return attn_kv4_kernel<D, 1, 2, true>;
+  if (nq == 3) return nt ? attn_kv4_kernel<D, 3, 1, true> : attn_kv4_kernel<D, 3, 1, false>;
+  if (ring == 1) return nt ? attn_kv4_kernel<D, 2, 1, true> : attn_kv4_kernel<D, 2, 1, false>;
+  return nt ? attn_kv4_kernel<D, 2, 2, true> : attn_kv4_kernel<D, 2, 2, false>;
 }
-Kv4Kernel pick_kv4(int D, int nq, int q_chunks) {
-  return D == 64 ? pick_kv4<64>(nq, q_chunks == 1) : pick_kv4<128>(nq, q_chunks == 1);
+Kv4Kernel pick_kv4(int D, int nq, int ring, int q_chunks) {
+  return D == 64 ? pick_kv4<64>(nq, ring, q_chunks == 1) : pick_kv4<128>(nq, ring, q_chunks == 1);
 }
 
 }  // namespace
@@ -403,17 +438,19 @@ int attention_kv4_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_r
   plan->nq = ((R + plan->q_chunks - 1) / plan->q_chunks + 15) / 16;
   const int cus = device_cu_count();
   if (cus <= 0) return SR_ELAUNCH;
-  const int per_cu = resident_per_cu((const void*)pick_kv4(D, plan->nq, plan->q_chunks), 64 * kWaves, 0);
   const long pairs = (long)B * Hkv * plan->q_chunks;
-  const long target = (long)cus * per_cu;
-  // Splits: the count, up to two workgroups per CU, whose time is least, in
-  // units of a key's time in a workgroup: the keys of a split times the workgroups
-  // that the busiest CU gets, plus the merge of each split's partial.
+  // Splits: the count whose time is least, in units of a key's time in a workgroup
+  // (two workgroups on a CU take little longer than one): the keys of a split,
+  // times the workgroups over two per CU, plus the merge of each split's partial.
+  // (32/8 heads of 128, gamma 5: one sequence of 32768 keys 230 us with 1 split, 26
+  // with 24, 31 with 48; 24 sequences of 256 to 8192 keys 65 with 1, 41 with 3 or 4, 50
+  // with 10; 16 sequences of 2048 24 with 1, 20 with 2 to 4, 33 with 8.)
   constexpr long kPerSplit = 64;
   const long most = (2L * cus + pairs - 1) / pairs;
   long splits = 1, best = 0;
   for (long n = 1; n <= most; ++n) {
-    const long t = (pairs * n + cus - 1) / cus * ((L + n - 1) / n) + (n > 1 ? n * kPerSplit : 0);
+    const long keys = (L + n - 1) / n;
+    const long t = (pairs * n > 2L * cus ? keys * pairs * n / (2L * cus) : keys) + (n > 1 ? n * kPerSplit : 0);
     if (n == 1 || t < best) best = t, splits = n;
   }
   const long max_splits = (L + kTile - 1) / kTile;
@@ -426,11 +463,20 @@ int attention_kv4_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_r
   plan->split_keys = sk;
   plan->n_splits = (L + sk - 1) / sk;
   plan->follow = 0;
+  // Tiles in flight per wave: two, but one with three row blocks, whose accumulators
+  // leave no registers for a second without keeping others in scratch (16 sequences of
+  // 2048 keys, 32/8 heads of 128, gamma 8: 22 us with one, 26 with two; 256 of 4096: 270
+  // and 287), and one with two row blocks and more than four workgroups per CU, for a
+  // third wave per SIMD (256 sequences of 2048 keys, gamma 5: 121 and 135; 24 ragged ones,
+  // 2.25 workgroups per CU: 46 and 39).
+  const long n_jobs = (long)plan->n_splits * pairs;
+  plan->ring = plan->nq == 3 || (plan->nq == 2 && n_jobs > 4L * cus) ? 1 : 2;
+  const long target =
+      (long)cus * resident_per_cu((const void*)pick_kv4(D, plan->nq, plan->ring, plan->q_chunks), 64 * kWaves, 0);
   // [arrival counters, one per 128-byte line][partial o][partial (m, l)][order]
   const size_t counters = (size_t)pairs * kCounterStride * sizeof(uint32_t);
   plan->part_offset = counters;
   size_t bytes = plan->n_splits > 1 ? counters + (size_t)B * Hkv * plan->n_splits * R * (D + 2) * sizeof(float) : 0;
-  const long n_jobs = (long)plan->n_splits * pairs;
   plan->ordered = n_jobs > target ? 1 : 0;
   plan->order_offset = (bytes + 15) / 16 * 16;
   if (plan->ordered) bytes = plan->order_offset + (size_t)n_jobs * sizeof(int32_t);
@@ -455,7 +501,7 @@ int launch_attention_kv4(const void* q, const void* k_codes, const void* k_power
                   (uint32_t*)workspace, order, B, gamma_max, Hq, Hkv, L_cap, window, sinks, scale * kLog2e,
                   plan.split_keys, plan.n_splits, plan.q_chunks, status};
   const dim3 grid((unsigned)((long)plan.n_splits * plan.q_chunks * B * Hkv));
-  hipLaunchKernelGGL(pick_kv4(D, plan.nq, plan.q_chunks), grid, dim3(64 * kWaves), 0, stream, a);
+  hipLaunchKernelGGL(pick_kv4(D, plan.nq, plan.ring, plan.q_chunks), grid, dim3(64 * kWaves), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SR_OK : SR_ELAUNCH;
 }
 
