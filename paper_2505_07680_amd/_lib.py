@@ -436,30 +436,53 @@ def specrouter_kv_compact(k_cache, v_cache, cache_mask, kv_len, status=None):
     _check(rc, "specrouter_kv_compact")
 
 
-def _here(*ts):
-    """All tensors on the current device (whose stream the call goes to)."""
-    cur = torch._C._cuda_getDevice()
-    for t in ts:
-        if t is not None and t.get_device() != cur:
-            raise ValueError("all tensors must be on the current HIP device")
+# The calls below make all their checks in one expression and look for the words
+# only when it fails: with a function call per tensor they took the host 2 to 5 us
+# more, which is what a call on one short sequence is bound by.
+
+def _current():
+    """The current device, whose stream a call goes to."""
+    return torch._C._cuda_getDevice()
 
 
-def _shaped(t, shape, dtype, name):
-    """t is a contiguous tensor of this shape and type."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}")
+def _refuse(where, **wanted):
+    """Raise for the first tensor that is not what a call wants: name=(tensor or
+    None, shape or None, dtypes or None, contiguous)."""
+    for name, (t, shape, dtypes, contiguous) in wanted.items():
+        if t is None:
+            continue
+        if t.get_device() != where:
+            raise ValueError(f"{name} must be on the current HIP device, as all tensors of a call")
+        if dtypes is not None and t.dtype not in dtypes:
+            raise TypeError(f"{name} must be one of {dtypes}, not {t.dtype}")
+        if shape is not None and t.shape != shape:
+            raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+        if contiguous and not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
 
 
-def _row_stride(t, name):
+def _vector(t, n, dtype, where):
+    """t is not a contiguous [n] of this type on this device."""
+    return t.shape != (n,) or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != where
+
+
+def _not_mask(t, B, L_cap, where):
+    return t.shape != (B, L_cap) or t.dtype not in _BYTE or not t.is_contiguous() or t.get_device() != where
+
+
+_BYTE = (torch.uint8, torch.int8, torch.bool)
+_OUT = (_BF16, torch.float32)
+
+
+def _row_stride(t, rows, H, D, name):
     """Elements from one row of t [B, rows, H, D] to the next, one stride for the whole batch."""
-    B, rows, H, D = t.shape
     s0, s1, s2, s3 = t.stride()
-    if t.dtype is not _BF16:
-        raise TypeError(f"{name} must be bfloat16")
-    row = s1 if rows > 1 else s0 if B > 1 else H * D
+    if s3 == 1 and s2 == D and s0 == rows * s1:
+        return s1
+    B = t.shape[0]
     if (D > 1 and s3 != 1) or (H > 1 and s2 != D) or (B > 1 and rows > 1 and s0 != rows * s1):
         raise ValueError(f"{name} must be [B, rows, H, D] with contiguous heads and evenly spaced rows")
-    return row
+    return s1 if rows > 1 else s0 if B > 1 else H * D
 
 
 def specrouter_qk_norm_rope(q, k, q_weight, k_weight, eps, rope_table, position, gamma, q_out, k_out,
@@ -468,45 +491,35 @@ def specrouter_qk_norm_rope(q, k, q_weight, k_weight, eps, rope_table, position,
     may be passed) -> q_out, k_out of the same shapes: every head normed (where
     its weight [D] is not None) and rotated to its position. rope_table fp32
     [max_positions, rot_dim] as from rope_table()."""
-    _here(q, k, q_weight, k_weight, rope_table, position, gamma, q_out, k_out, status)
-    B, rows, Hq, D = q.shape
-    Hkv = k.shape[2]
-    if k.shape != (B, rows, Hkv, D):
-        raise ValueError("q [B, rows, Hq, D] and k [B, rows, Hkv, D] expected")
-    _shaped(q_out, q.shape, _BF16, "q_out")
-    _shaped(k_out, k.shape, _BF16, "k_out")
-    _shaped(position, (B,), _INT32, "position")
-    _shaped(gamma, (B,), _INT32, "gamma")
-    code = SR_BF16
-    for w, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            _shaped(w, (D,), w.dtype, n)
-            code = logits_dtype_code(w)
-    if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
-        raise TypeError("q_weight and k_weight must share a dtype")
-    if rope_table.dim() != 2:
-        raise ValueError("rope_table must be [max_positions, rot_dim]")
-    _shaped(rope_table, rope_table.shape, torch.float32, "rope_table")
+    here = _current()
+    B, rows, Hq, D = qs = q.shape
+    ks = k.shape
+    max_positions, rot = rope_table.shape
+    w = q_weight if q_weight is not None else k_weight
+    code = SR_BF16 if w is None or w.dtype is _BF16 else SR_F32
+    if (not (q.get_device() == k.get_device() == rope_table.get_device() == position.get_device() == gamma.get_device()
+             == q_out.get_device() == k_out.get_device() == here)
+            or len(ks) != 4 or ks[0] != B or ks[1] != rows or ks[3] != D
+            or not (q.dtype is k.dtype is q_out.dtype is k_out.dtype is _BF16)
+            or q_out.shape != qs or k_out.shape != ks or not q_out.is_contiguous() or not k_out.is_contiguous()
+            or not (position.dtype is gamma.dtype is _INT32) or position.numel() != B or gamma.numel() != B
+            or position.dim() != 1 or gamma.dim() != 1 or not position.is_contiguous() or not gamma.is_contiguous()
+            or rope_table.dtype is not torch.float32 or not rope_table.is_contiguous()
+            or q_weight is not None and _vector(q_weight, D, w.dtype, here)
+            or k_weight is not None and _vector(k_weight, D, w.dtype, here)
+            or w is not None and w.dtype not in _OUT or status is not None and status.get_device() != here):
+        _refuse(here, q=(q, None, (_BF16,), False), k=(k, (B, rows, ks[2], D), (_BF16,), False),
+                q_out=(q_out, qs, (_BF16,), True), k_out=(k_out, ks, (_BF16,), True),
+                position=(position, (B,), (_INT32,), True), gamma=(gamma, (B,), (_INT32,), True),
+                rope_table=(rope_table, None, (torch.float32,), True),
+                q_weight=(q_weight, (D,), _OUT, True),
+                k_weight=(k_weight, (D,), (w.dtype,) if w is not None else None, True), status=(status, None, (_INT32,), True))
     rc = load().specrouter_qk_norm_rope(
-        q.data_ptr(), _row_stride(q, "q"), k.data_ptr(), _row_stride(k, "k"), _ptr(q_weight), _ptr(k_weight), code,
-        float(eps), rope_table.data_ptr(), rope_table.shape[0], rope_table.shape[1], 1 if interleaved else 0,
-        position.data_ptr(), gamma.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), B, rows - 1, Hq, Hkv, D,
-        _ptr(status), _stream())
-    _check(rc, "specrouter_qk_norm_rope")
-
-
-def _kv4_shapes(k_codes, k_powers, v_codes, v_powers, B, Hkv, D):
-    L_cap = k_codes.shape[2] if k_codes.dim() == 4 else -1
-    for t, w, n in ((k_codes, D // 2, "k_codes"), (k_powers, D // 32, "k_powers"), (v_codes, D // 2, "v_codes"),
-                    (v_powers, D // 32, "v_powers")):
-        _shaped(t, (B, Hkv, L_cap, w), torch.uint8, n)
-    return L_cap
-
-
-def _mask_of(cache_mask, B, L_cap):
-    if cache_mask is not None and (cache_mask.shape != (B, L_cap) or cache_mask.element_size() != 1
-                                   or not cache_mask.is_contiguous()):
-        raise ValueError("cache_mask must be u8 [B, L_cap]")
+        q.data_ptr(), _row_stride(q, rows, Hq, D, "q"), k.data_ptr(), _row_stride(k, rows, ks[2], D, "k"), _ptr(q_weight), _ptr(k_weight), code,
+        eps, rope_table.data_ptr(), max_positions, rot, 1 if interleaved else 0, position.data_ptr(), gamma.data_ptr(),
+        q_out.data_ptr(), k_out.data_ptr(), B, rows - 1, Hq, ks[2], D, _ptr(status), _stream())
+    if rc:
+        _check(rc, "specrouter_qk_norm_rope")
 
 
 def specrouter_kv4_append(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_powers, cache_mask, kv_len,
@@ -514,26 +527,43 @@ def specrouter_kv4_append(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_pow
     """k_new/v_new [B, rows, Hkv, D] bf16 -> the 4-bit cache (codes
     [B, Hkv, L_cap, D/2], powers [B, Hkv, L_cap, D/32], u8) at each cursor;
     k_seen/v_seen [B, rows, Hkv, D] bf16: the rows as the cache now holds them."""
-    _here(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_powers, cache_mask, kv_len, shared_len, k_seen, v_seen,
-          status)
-    B, rows, Hkv, D = k_new.shape
-    if v_new.shape != k_new.shape:
-        raise ValueError("k_new and v_new must be [B, rows, Hkv, D]")
-    L_cap = _kv4_shapes(k_codes, k_powers, v_codes, v_powers, B, Hkv, D)
-    _mask_of(cache_mask, B, L_cap)
-    _shaped(gamma, (B,), _INT32, "gamma")
-    _shaped(kv_len, (B,), _INT32, "kv_len")
-    if shared_len is not None:
-        _shaped(shared_len, (1,), _INT32, "shared_len")
-    for t, n in ((k_seen, "k_seen"), (v_seen, "v_seen")):
-        if t is not None:
-            _shaped(t, k_new.shape, _BF16, n)
+    here = _current()
+    B, rows, Hkv, D = ns = k_new.shape
+    cs, ps = k_codes.shape, k_powers.shape
+    L_cap = cs[2] if len(cs) == 4 else -1
+    if (not (k_new.get_device() == v_new.get_device() == gamma.get_device() == kv_len.get_device()
+             == k_codes.get_device() == k_powers.get_device() == v_codes.get_device() == v_powers.get_device() == here)
+            or v_new.shape != ns or not (k_new.dtype is v_new.dtype is _BF16)
+            or cs != (B, Hkv, L_cap, D // 2) or ps != (B, Hkv, L_cap, D // 32) or v_codes.shape != cs
+            or v_powers.shape != ps
+            or not (k_codes.dtype is k_powers.dtype is v_codes.dtype is v_powers.dtype is torch.uint8)
+            or not (k_codes.is_contiguous() and k_powers.is_contiguous() and v_codes.is_contiguous()
+                    and v_powers.is_contiguous() and gamma.is_contiguous() and kv_len.is_contiguous())
+            or not (gamma.dtype is kv_len.dtype is _INT32) or gamma.numel() != B or kv_len.numel() != B
+            or gamma.dim() != 1 or kv_len.dim() != 1
+            or k_seen is not None and (k_seen.shape != ns or k_seen.dtype is not _BF16 or not k_seen.is_contiguous()
+                                       or k_seen.get_device() != here)
+            or v_seen is not None and (v_seen.shape != ns or v_seen.dtype is not _BF16 or not v_seen.is_contiguous()
+                                       or v_seen.get_device() != here)
+            or cache_mask is not None and _not_mask(cache_mask, B, L_cap, here)
+            or shared_len is not None and _vector(shared_len, 1, _INT32, here)
+            or status is not None and status.get_device() != here):
+        _refuse(here, k_new=(k_new, None, (_BF16,), False), v_new=(v_new, ns, (_BF16,), False),
+                k_codes=(k_codes, (B, Hkv, L_cap, D // 2), (torch.uint8,), True),
+                k_powers=(k_powers, (B, Hkv, L_cap, D // 32), (torch.uint8,), True),
+                v_codes=(v_codes, (B, Hkv, L_cap, D // 2), (torch.uint8,), True),
+                v_powers=(v_powers, (B, Hkv, L_cap, D // 32), (torch.uint8,), True),
+                cache_mask=(cache_mask, (B, L_cap), _BYTE, True), gamma=(gamma, (B,), (_INT32,), True),
+                kv_len=(kv_len, (B,), (_INT32,), True), shared_len=(shared_len, (1,), (_INT32,), True),
+                k_seen=(k_seen, ns, (_BF16,), True), v_seen=(v_seen, ns, (_BF16,), True),
+                status=(status, None, (_INT32,), True))
     rc = load().specrouter_kv4_append(
-        k_new.data_ptr(), _row_stride(k_new, "k_new"), v_new.data_ptr(), _row_stride(v_new, "v_new"), gamma.data_ptr(),
+        k_new.data_ptr(), _row_stride(k_new, rows, Hkv, D, "k_new"), v_new.data_ptr(), _row_stride(v_new, rows, Hkv, D, "v_new"), gamma.data_ptr(),
         k_codes.data_ptr(), k_powers.data_ptr(), v_codes.data_ptr(), v_powers.data_ptr(), _ptr(cache_mask),
         kv_len.data_ptr(), _ptr(shared_len), _ptr(k_seen), _ptr(v_seen), B, rows - 1, Hkv, D, L_cap, _ptr(status),
         _stream())
-    _check(rc, "specrouter_kv4_append")
+    if rc:
+        _check(rc, "specrouter_kv4_append")
 
 
 def specrouter_verify_attention_window_workspace_size(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks) -> int:
@@ -544,36 +574,44 @@ def specrouter_verify_attention_kv4_workspace_size(B, gamma_max, Hq, Hkv, D, L_c
     return load().specrouter_verify_attention_kv4_workspace_size(B, gamma_max, Hq, Hkv, D, L_cap, window, sinks)
 
 
-def _out_code(out, shape):
-    if out.shape != shape or not out.is_contiguous():
-        raise ValueError("out must be contiguous [B, gamma_max+1, Hq, D]")
-    if out.dtype is _BF16:
-        return SR_BF16
-    if out.dtype is torch.float32:
-        return SR_F32
-    raise TypeError("out must be float32 or bfloat16")
+def _bytes_of(workspace, here):
+    if workspace is None:
+        return 0
+    if workspace.get_device() != here or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the current HIP device")
+    return workspace.numel() * workspace.element_size()
 
 
 def specrouter_verify_attention_window(q, k_cache, v_cache, cache_mask, kv_len, gamma, out, scale, window, sinks=0,
                                        workspace=None, status=None):
     """specrouter_verify_attention where a row sees the last `window` cache rows
     up to its own and the first `sinks`; out [B, gmax+1, Hq, D] fp32 or bf16."""
-    _here(q, k_cache, v_cache, cache_mask, kv_len, gamma, out, workspace, status)
-    B, G1, Hq, D = q.shape
-    Hkv, L_cap = k_cache.shape[1], k_cache.shape[2]
-    _shaped(q, q.shape, _BF16, "q")
-    _shaped(k_cache, (B, Hkv, L_cap, D), _BF16, "k_cache")
-    _shaped(v_cache, (B, Hkv, L_cap, D), _BF16, "v_cache")
-    _shaped(kv_len, (B,), _INT32, "kv_len")
-    _shaped(gamma, (B,), _INT32, "gamma")
-    _mask_of(cache_mask, B, L_cap)
-    code = _out_code(out, q.shape)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    here = _current()
+    B, G1, Hq, D = qs = q.shape
+    cs = k_cache.shape
+    Hkv, L_cap = cs[1], cs[2]
+    out_bf16 = out.dtype is _BF16
+    if (not (q.get_device() == k_cache.get_device() == v_cache.get_device() == kv_len.get_device()
+             == gamma.get_device() == out.get_device() == here)
+            or len(cs) != 4 or cs[0] != B or cs[3] != D or v_cache.shape != cs or out.shape != qs
+            or not (q.dtype is k_cache.dtype is v_cache.dtype is _BF16)
+            or not (out_bf16 or out.dtype is torch.float32)
+            or not (q.is_contiguous() and k_cache.is_contiguous() and v_cache.is_contiguous() and out.is_contiguous()
+                    and kv_len.is_contiguous() and gamma.is_contiguous())
+            or not (gamma.dtype is kv_len.dtype is _INT32) or gamma.numel() != B or kv_len.numel() != B
+            or gamma.dim() != 1 or kv_len.dim() != 1
+            or cache_mask is not None and _not_mask(cache_mask, B, L_cap, here)
+            or status is not None and status.get_device() != here):
+        _refuse(here, q=(q, None, (_BF16,), True), k_cache=(k_cache, (B, Hkv, L_cap, D), (_BF16,), True),
+                v_cache=(v_cache, (B, Hkv, L_cap, D), (_BF16,), True), cache_mask=(cache_mask, (B, L_cap), _BYTE, True),
+                kv_len=(kv_len, (B,), (_INT32,), True), gamma=(gamma, (B,), (_INT32,), True),
+                out=(out, qs, _OUT, True), status=(status, None, (_INT32,), True))
     rc = load().specrouter_verify_attention_window(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(cache_mask), kv_len.data_ptr(), gamma.data_ptr(),
-        out.data_ptr(), code, B, G1 - 1, Hq, Hkv, D, L_cap, int(window), int(sinks), float(scale), _ptr(workspace),
-        ws_bytes, _ptr(status), _stream())
-    _check(rc, "specrouter_verify_attention_window")
+        out.data_ptr(), SR_BF16 if out_bf16 else SR_F32, B, G1 - 1, Hq, Hkv, D, L_cap, window, sinks, scale,
+        _ptr(workspace), _bytes_of(workspace, here), _ptr(status), _stream())
+    if rc:
+        _check(rc, "specrouter_verify_attention_window")
     return out
 
 
@@ -582,21 +620,37 @@ def specrouter_verify_attention_kv4(q, k_codes, k_powers, v_codes, v_powers, cac
     """The attention over a 4-bit cache (codes [B, Hkv, L_cap, D/2], powers
     [B, Hkv, L_cap, D/32], u8), of all keys (window 0) or a window and sinks;
     out [B, gmax+1, Hq, D] fp32 or bf16."""
-    _here(q, k_codes, k_powers, v_codes, v_powers, cache_mask, kv_len, gamma, out, workspace, status)
-    B, G1, Hq, D = q.shape
-    Hkv = k_codes.shape[1]
-    _shaped(q, q.shape, _BF16, "q")
-    L_cap = _kv4_shapes(k_codes, k_powers, v_codes, v_powers, B, Hkv, D)
-    _shaped(kv_len, (B,), _INT32, "kv_len")
-    _shaped(gamma, (B,), _INT32, "gamma")
-    _mask_of(cache_mask, B, L_cap)
-    code = _out_code(out, q.shape)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    here = _current()
+    B, G1, Hq, D = qs = q.shape
+    cs, ps = k_codes.shape, k_powers.shape
+    Hkv, L_cap = cs[1], cs[2]
+    out_bf16 = out.dtype is _BF16
+    if (not (q.get_device() == k_codes.get_device() == k_powers.get_device() == v_codes.get_device()
+             == v_powers.get_device() == kv_len.get_device() == gamma.get_device() == out.get_device() == here)
+            or cs != (B, Hkv, L_cap, D // 2) or ps != (B, Hkv, L_cap, D // 32) or v_codes.shape != cs
+            or v_powers.shape != ps or out.shape != qs or q.dtype is not _BF16
+            or not (k_codes.dtype is k_powers.dtype is v_codes.dtype is v_powers.dtype is torch.uint8)
+            or not (out_bf16 or out.dtype is torch.float32)
+            or not (q.is_contiguous() and k_codes.is_contiguous() and k_powers.is_contiguous()
+                    and v_codes.is_contiguous() and v_powers.is_contiguous() and out.is_contiguous()
+                    and kv_len.is_contiguous() and gamma.is_contiguous())
+            or not (gamma.dtype is kv_len.dtype is _INT32) or gamma.numel() != B or kv_len.numel() != B
+            or gamma.dim() != 1 or kv_len.dim() != 1
+            or cache_mask is not None and _not_mask(cache_mask, B, L_cap, here)
+            or status is not None and status.get_device() != here):
+        _refuse(here, q=(q, None, (_BF16,), True), k_codes=(k_codes, (B, Hkv, L_cap, D // 2), (torch.uint8,), True),
+                k_powers=(k_powers, (B, Hkv, L_cap, D // 32), (torch.uint8,), True),
+                v_codes=(v_codes, (B, Hkv, L_cap, D // 2), (torch.uint8,), True),
+                v_powers=(v_powers, (B, Hkv, L_cap, D // 32), (torch.uint8,), True),
+                cache_mask=(cache_mask, (B, L_cap), _BYTE, True), kv_len=(kv_len, (B,), (_INT32,), True),
+                gamma=(gamma, (B,), (_INT32,), True), out=(out, qs, _OUT, True), status=(status, None, (_INT32,), True))
     rc = load().specrouter_verify_attention_kv4(
         q.data_ptr(), k_codes.data_ptr(), k_powers.data_ptr(), v_codes.data_ptr(), v_powers.data_ptr(),
-        _ptr(cache_mask), kv_len.data_ptr(), gamma.data_ptr(), out.data_ptr(), code, B, G1 - 1, Hq, Hkv, D, L_cap,
-        int(window), int(sinks), float(scale), _ptr(workspace), ws_bytes, _ptr(status), _stream())
-    _check(rc, "specrouter_verify_attention_kv4")
+        _ptr(cache_mask), kv_len.data_ptr(), gamma.data_ptr(), out.data_ptr(), SR_BF16 if out_bf16 else SR_F32, B,
+        G1 - 1, Hq, Hkv, D, L_cap, window, sinks, scale, _ptr(workspace), _bytes_of(workspace, here), _ptr(status),
+        _stream())
+    if rc:
+        _check(rc, "specrouter_verify_attention_kv4")
     return out
 
 
