@@ -10,6 +10,7 @@ namespace {
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;  // key streams
 // How far (log2) a tile's maximum exceeds a row's softmax reference before that
@@ -66,6 +67,15 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   const __bf16 b = (__bf16)hi;
   return (uint32_t)__builtin_bit_cast(uint16_t, a) | ((uint32_t)__builtin_bit_cast(uint16_t, b) << 16);
 }
+
+// (the same in one instruction)
+__device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{lo, hi}, bf16x2));
+}
+
+// A branch that is seldom taken: its code goes out of the way (a taken branch
+// costs a wave about 45 cycles).
+__device__ __forceinline__ bool rare(bool x) { return __builtin_expect(x, 0); }
 
 // Order LDS accesses of one wave around a point (compiler barrier; the LDS
 // unit serves one wave's requests in order).
@@ -330,7 +340,8 @@ __device__ __forceinline__ void merge_and_store(unsigned char* lds, const floatx
       const float Mo = d == 1 ? perm_f32<dpp::kXor1>(M) : perm_f32<dpp::kXor2>(M);
       const float Do = d == 1 ? perm_f32<dpp::kXor1>(den) : perm_f32<dpp::kXor2>(den);
       const float Mn = fmaxf(M, Mo);
-      den = Mn == kNegInf ? 0.f : den * exp2_hw(M - Mn) + Do * exp2_hw(Mo - Mn);
+      // (the fused operand is written out, so that every kernel rounds alike)
+      den = Mn == kNegInf ? 0.f : fmaf(den, exp2_hw(M - Mn), Do * exp2_hw(Mo - Mn));
       M = Mn;
     }
     if (tid % 4 == 0) {

@@ -33,8 +33,6 @@
 namespace sr {
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
 constexpr int kTile = 32;   // keys per tile of a wave
 constexpr int kMaxNQ4 = 3;  // 16-row query blocks per wave: more than 48 rows go to further query chunks
 constexpr int kMergeMost4 = 49152;  // the merge's LDS: three workgroups fit a CU's
@@ -62,14 +60,6 @@ __device__ __forceinline__ u32x4 widen(uint32_t codes, float scale) {
   v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
   return v;
 }
-
-__device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{lo, hi}, bf16x2));
-}
-
-// A branch that is seldom taken: its code goes out of the way (a taken branch
-// costs a wave about 45 cycles).
-__device__ __forceinline__ bool rare(bool x) { return __builtin_expect(x, 0); }
 
 // Where 16-byte chunk c of V row r sits in its row.
 __device__ __forceinline__ int chunk_at(int c, int r) { return c ^ (((r & 3) << 1) | ((r >> 2) & 1)); }
