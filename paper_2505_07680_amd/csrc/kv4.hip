@@ -15,7 +15,7 @@
 // nearest even). A wave takes consecutive positions of one head, so that its
 // stores are one run of the head's slab.
 
-#include "sr_internal.h"
+#include "caching.h"
 
 namespace sr {
 namespace {
@@ -85,7 +85,7 @@ __device__ __forceinline__ Span span_of(const Append4& a, int b) {
 
 // Rows [first, first + kU * step) in steps of the sequence's n Hkv rows, head by
 // head; a lane takes its eight elements of every one (kU loads of K and V in flight).
-template <int D, int kU>
+template <int D, int kU, int CACHING>
 __device__ __forceinline__ void append_rows(const Append4& a, int b, int cur, int n, int first, int step, int total) {
   constexpr int kLanes = D / 8;
   const int c = (int)(threadIdx.x % kLanes);
@@ -97,8 +97,8 @@ __device__ __forceinline__ void append_rows(const Append4& a, int b, int cur, in
     h[u] = row / n;
     i[u] = row - h[u] * n;
     const int64_t token = (int64_t)b * (a.gmax + 1) + i[u];
-    kr[u] = *(const u32x4*)(a.k_new + token * a.k_stride + (int64_t)h[u] * D + c * 8);
-    vr[u] = *(const u32x4*)(a.v_new + token * a.v_stride + (int64_t)h[u] * D + c * 8);
+    kr[u] = load_once<CACHING>(a.k_new + token * a.k_stride + (int64_t)h[u] * D + c * 8);
+    vr[u] = load_once<CACHING>(a.v_new + token * a.v_stride + (int64_t)h[u] * D + c * 8);
   }
 #pragma unroll
   for (int u = 0; u < kU; ++u) {
@@ -112,8 +112,8 @@ __device__ __forceinline__ void append_rows(const Append4& a, int b, int cur, in
         a.v_powers[slot * (D / 32) + c / 4] = (uint8_t)v4.power;
       }
       const int64_t seen = ((((int64_t)b * (a.gmax + 1) + i[u]) * a.Hkv + h[u]) * D) + c * 8;
-      if (a.k_seen) *(u32x4*)(a.k_seen + seen) = values_of(k4);
-      if (a.v_seen) *(u32x4*)(a.v_seen + seen) = values_of(v4);
+      if (a.k_seen) store_once<CACHING>(a.k_seen + seen, values_of(k4));
+      if (a.v_seen) store_once<CACHING>(a.v_seen + seen, values_of(v4));
     }
   }
 }
@@ -134,7 +134,7 @@ kv4_append_step_kernel(Append4 a) {
   }
   const int total = s.n * a.Hkv;
   for (int first = (int)threadIdx.x / (D / 8); first < total; first += kRows)
-    append_rows<D, 1>(a, b, s.cur, s.n, first, kRows, total);
+    append_rows<D, 1, kKeep>(a, b, s.cur, s.n, first, kRows, total);
   if (a.mask)
     for (int i = threadIdx.x; i < s.n; i += kStepThreads) a.mask[(int64_t)b * a.L_cap + s.cur + i] = 1;
   if (threadIdx.x == 0) a.kv_len[b] = s.cur + s.n;
@@ -146,7 +146,7 @@ constexpr int kPromptThreads = 256;
 constexpr int kPromptUnroll = 4;
 template <int D>
 constexpr int prompt_rows() { return kPromptThreads / (D / 8) * kPromptUnroll; }
-template <int D>
+template <int D, int CACHING>
 __global__ void __launch_bounds__(kPromptThreads)
 kv4_append_prompt_kernel(Append4 a, int blocks_per_seq) {
   constexpr int kRows = 64 / (D / 8);  // rows of a wave at a time
@@ -157,7 +157,7 @@ kv4_append_prompt_kernel(Append4 a, int blocks_per_seq) {
   const int lane = threadIdx.x & 63;
   const int first = blk * prompt_rows<D>() + wave_id() * (kRows * kPromptUnroll);
   if (first >= total) return;
-  append_rows<D, kPromptUnroll>(a, b, s.cur, s.n, first + lane / (D / 8), kRows, total);
+  append_rows<D, kPromptUnroll, CACHING>(a, b, s.cur, s.n, first + lane / (D / 8), kRows, total);
 }
 
 constexpr int kLenThreads = 256;
@@ -173,6 +173,11 @@ kv4_append_length_kernel(Append4 a) {
   if (a.mask)
     for (int i = threadIdx.x; i < s.n; i += kLenThreads) a.mask[(int64_t)b * a.L_cap + s.cur + i] = 1;
   if (threadIdx.x == 0) a.kv_len[b] = s.cur + s.n;
+}
+
+template <int CACHING>
+auto prompt_kernel(int D) {
+  return D == 64 ? kv4_append_prompt_kernel<64, CACHING> : kv4_append_prompt_kernel<128, CACHING>;
 }
 
 }  // namespace
@@ -195,8 +200,10 @@ int launch_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, in
   }
   const int per = D == 64 ? prompt_rows<64>() : prompt_rows<128>();
   const int blocks = (int)((rows + per - 1) / per);
-  hipLaunchKernelGGL(D == 64 ? kv4_append_prompt_kernel<64> : kv4_append_prompt_kernel<128>,
-                     dim3((unsigned)((long)B * blocks)), dim3(kPromptThreads), 0, stream, a, blocks);
+  const Caching caching = caching_of((long)B * rows * D * 4 * (k_seen || v_seen ? 2 : 1));
+  const auto kernel = caching == kPass ? prompt_kernel<kPass>(D)
+                                       : caching == kReadOnce ? prompt_kernel<kReadOnce>(D) : prompt_kernel<kKeep>(D);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((long)B * blocks)), dim3(kPromptThreads), 0, stream, a, blocks);
   if (hipGetLastError() != hipSuccess) return SR_ELAUNCH;
   hipLaunchKernelGGL(kv4_append_length_kernel, dim3(B), dim3(kLenThreads), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SR_OK : SR_ELAUNCH;

@@ -16,7 +16,7 @@
 // used. With pairs half a rotation apart the partner's values come from the
 // lane that holds them, by way of the LDS crossbar.
 
-#include "sr_internal.h"
+#include "caching.h"
 
 namespace sr {
 namespace {
@@ -51,7 +51,7 @@ __device__ __forceinline__ void load_weights(const void* w, bool f32, int c8, fl
   }
 }
 
-template <int D, bool ADJACENT>
+template <int D, bool ADJACENT, int CACHING>
 __global__ void __launch_bounds__(kRopeThreads)
 qk_norm_rope_kernel(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride,
                     const void* __restrict__ qw, const void* __restrict__ kw, bool w_f32, float eps,
@@ -85,7 +85,7 @@ qk_norm_rope_kernel(const uint16_t* q, int64_t q_stride, const uint16_t* k, int6
   for (int s = 0; s < kHeadSteps; ++s) {
     const int h = min(h0 + s * kHeads, H - 1);
     const uint16_t* src = h < Hq ? q + token * q_stride + (int64_t)h * D : k + token * k_stride + (int64_t)(h - Hq) * D;
-    x[s] = *(const u32x4*)(src + c * 8);
+    x[s] = load_once<CACHING>(src + c * 8);
   }
   float wq[8], wk[8];
   if (qw) load_weights(qw, w_f32, c * 8, wq);
@@ -144,10 +144,16 @@ qk_norm_rope_kernel(const uint16_t* q, int64_t q_stride, const uint16_t* k, int6
     }
     if (h < H) {
       uint16_t* dst = is_q ? q_out + (token * Hq + h) * D : k_out + (token * Hkv + (h - Hq)) * D;
-      *(u32x4*)(dst + c * 8) =
-          u32x4{to_bf16x2(z[0], z[1]), to_bf16x2(z[2], z[3]), to_bf16x2(z[4], z[5]), to_bf16x2(z[6], z[7])};
+      store_once<CACHING>(dst + c * 8, u32x4{to_bf16x2(z[0], z[1]), to_bf16x2(z[2], z[3]), to_bf16x2(z[4], z[5]),
+                                             to_bf16x2(z[6], z[7])});
     }
   }
+}
+
+template <int CACHING>
+auto rope_kernel(int D, bool adjacent) {
+  return D == 64 ? (adjacent ? qk_norm_rope_kernel<64, true, CACHING> : qk_norm_rope_kernel<64, false, CACHING>)
+                 : (adjacent ? qk_norm_rope_kernel<128, true, CACHING> : qk_norm_rope_kernel<128, false, CACHING>);
 }
 
 }  // namespace
@@ -160,8 +166,10 @@ int launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t 
   const int parts = (Hq + Hkv + per_wave - 1) / per_wave;
   const long n_items = (long)B * (gamma_max + 1) * parts;
   const long blocks = (n_items + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
-  const auto kernel = D == 64 ? (adjacent ? qk_norm_rope_kernel<64, true> : qk_norm_rope_kernel<64, false>)
-                              : (adjacent ? qk_norm_rope_kernel<128, true> : qk_norm_rope_kernel<128, false>);
+  const Caching caching = caching_of((long)B * (gamma_max + 1) * (Hq + Hkv) * D * 4);
+  const auto kernel = caching == kPass ? rope_kernel<kPass>(D, adjacent)
+                                       : caching == kReadOnce ? rope_kernel<kReadOnce>(D, adjacent)
+                                                              : rope_kernel<kKeep>(D, adjacent);
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRopeThreads), 0, stream, (const uint16_t*)q, q_stride,
                      (const uint16_t*)k, k_stride, q_weight, k_weight, w_f32, eps, table, max_positions, rot, position,
                      gamma, (uint16_t*)q_out, (uint16_t*)k_out, gamma_max, Hq, Hkv, parts, (uint32_t)n_items, status);
