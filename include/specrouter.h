@@ -141,7 +141,9 @@ int specrouter_verify_attention(const void* q, const void* k_cache, const void* 
  * j < sinks. Positions are cache rows, masked ones counted. Only the rows that
  * some new row can see are read: at most window + gamma_b + sinks per sequence
  * and kv head, and what lies between the sinks and the window is ignored
- * whatever it holds.
+ * whatever it holds. NaN or infinity among a row's own keys and values gives NaN
+ * in that row; in V of a key that some new row sees it may give NaN in the
+ * sequence's other rows too, as 0 times it is NaN.
  *
  * window     >= 1 (from L_cap on it hides nothing); sinks >= 0; else SR_EINVAL
  * out        [B][gamma_max+1][Hq][D] of out_dtype: SR_F32, or SR_BF16 (the same
@@ -436,7 +438,8 @@ int specrouter_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
  * k_seen, v_seen  bf16 [B][gamma_max+1][Hkv][D] out, or NULL each: the rows as
  *               the cache now holds them, for attention among a prompt's own
  *               rows. Rows i > gamma_b and those of an untouched sequence are
- *               not written
+ *               not written. May be k_new / v_new themselves where those are
+ *               contiguous, else they must not overlap any other argument
  * shared_len    i32 [1] or NULL, not an element of kv_len
  * Everything else as for specrouter_kv_append; lengths, mask and rollback of
  * such a cache are those of a bf16 one.
@@ -449,7 +452,8 @@ int specrouter_kv4_append(const void* k_new, int64_t k_stride, const void* v_new
 /* Verification attention over such a cache: specrouter_verify_attention (window
  * 0) or specrouter_verify_attention_window (window >= 1) with K and V the values
  * that codes and powers stand for, which the products take exactly. Entries that
- * no new row sees are ignored whatever they hold. out_dtype as for the window
+ * no new row sees are ignored whatever they hold (NaN in V that one row sees: as
+ * for the window call). out_dtype as for the window
  * call; workspace of specrouter_verify_attention_kv4_workspace_size() bytes for
  * the same arguments, zero-filled before its first use.
  */

@@ -446,8 +446,8 @@ def _current():
 
 
 def _refuse(where, **wanted):
-    """Raise for the first tensor that is not what a call wants: name=(tensor or
-    None, shape or None, dtypes or None, contiguous)."""
+    """Raise, naming the first tensor that is not what a call wants: name=(tensor
+    or None, shape or None, dtypes or None, contiguous)."""
     for name, (t, shape, dtypes, contiguous) in wanted.items():
         if t is None:
             continue
@@ -459,6 +459,7 @@ def _refuse(where, **wanted):
             raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
         if contiguous and not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
+    raise ValueError("the call's tensors do not fit each other, or a size is out of range")
 
 
 def _vector(t, n, dtype, where):
@@ -470,6 +471,11 @@ def _not_mask(t, B, L_cap, where):
     return t.shape != (B, L_cap) or t.dtype not in _BYTE or not t.is_contiguous() or t.get_device() != where
 
 
+def _not_word(t, where):
+    return t.dtype is not _INT32 or t.get_device() != where
+
+
+_INT_MAX = 0x7fffffff  # (a C int: ctypes would drop the bits above)
 _BYTE = (torch.uint8, torch.int8, torch.bool)
 _OUT = (_BF16, torch.float32)
 
@@ -493,13 +499,13 @@ def specrouter_qk_norm_rope(q, k, q_weight, k_weight, eps, rope_table, position,
     [max_positions, rot_dim] as from rope_table()."""
     here = _current()
     B, rows, Hq, D = qs = q.shape
-    ks = k.shape
+    Bk, rows_k, Hkv, Dk = ks = k.shape
     max_positions, rot = rope_table.shape
     w = q_weight if q_weight is not None else k_weight
     code = SR_BF16 if w is None or w.dtype is _BF16 else SR_F32
     if (not (q.get_device() == k.get_device() == rope_table.get_device() == position.get_device() == gamma.get_device()
              == q_out.get_device() == k_out.get_device() == here)
-            or len(ks) != 4 or ks[0] != B or ks[1] != rows or ks[3] != D
+            or Bk != B or rows_k != rows or Dk != D or max_positions > _INT_MAX
             or not (q.dtype is k.dtype is q_out.dtype is k_out.dtype is _BF16)
             or q_out.shape != qs or k_out.shape != ks or not q_out.is_contiguous() or not k_out.is_contiguous()
             or not (position.dtype is gamma.dtype is _INT32) or position.numel() != B or gamma.numel() != B
@@ -507,17 +513,17 @@ def specrouter_qk_norm_rope(q, k, q_weight, k_weight, eps, rope_table, position,
             or rope_table.dtype is not torch.float32 or not rope_table.is_contiguous()
             or q_weight is not None and _vector(q_weight, D, w.dtype, here)
             or k_weight is not None and _vector(k_weight, D, w.dtype, here)
-            or w is not None and w.dtype not in _OUT or status is not None and status.get_device() != here):
-        _refuse(here, q=(q, None, (_BF16,), False), k=(k, (B, rows, ks[2], D), (_BF16,), False),
+            or w is not None and w.dtype not in _OUT or status is not None and _not_word(status, here)):
+        _refuse(here, q=(q, None, (_BF16,), False), k=(k, (B, rows, Hkv, D), (_BF16,), False),
                 q_out=(q_out, qs, (_BF16,), True), k_out=(k_out, ks, (_BF16,), True),
                 position=(position, (B,), (_INT32,), True), gamma=(gamma, (B,), (_INT32,), True),
                 rope_table=(rope_table, None, (torch.float32,), True),
                 q_weight=(q_weight, (D,), _OUT, True),
-                k_weight=(k_weight, (D,), (w.dtype,) if w is not None else None, True), status=(status, None, (_INT32,), True))
+                k_weight=(k_weight, (D,), _OUT if q_weight is None else (w.dtype,), True), status=(status, None, (_INT32,), True))
     rc = load().specrouter_qk_norm_rope(
-        q.data_ptr(), _row_stride(q, rows, Hq, D, "q"), k.data_ptr(), _row_stride(k, rows, ks[2], D, "k"), _ptr(q_weight), _ptr(k_weight), code,
+        q.data_ptr(), _row_stride(q, rows, Hq, D, "q"), k.data_ptr(), _row_stride(k, rows, Hkv, D, "k"), _ptr(q_weight), _ptr(k_weight), code,
         eps, rope_table.data_ptr(), max_positions, rot, 1 if interleaved else 0, position.data_ptr(), gamma.data_ptr(),
-        q_out.data_ptr(), k_out.data_ptr(), B, rows - 1, Hq, ks[2], D, _ptr(status), _stream())
+        q_out.data_ptr(), k_out.data_ptr(), B, rows - 1, Hq, Hkv, D, _ptr(status), _stream())
     if rc:
         _check(rc, "specrouter_qk_norm_rope")
 
@@ -529,8 +535,8 @@ def specrouter_kv4_append(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_pow
     k_seen/v_seen [B, rows, Hkv, D] bf16: the rows as the cache now holds them."""
     here = _current()
     B, rows, Hkv, D = ns = k_new.shape
-    cs, ps = k_codes.shape, k_powers.shape
-    L_cap = cs[2] if len(cs) == 4 else -1
+    _, _, L_cap, _ = cs = k_codes.shape
+    ps = k_powers.shape
     if (not (k_new.get_device() == v_new.get_device() == gamma.get_device() == kv_len.get_device()
              == k_codes.get_device() == k_powers.get_device() == v_codes.get_device() == v_powers.get_device() == here)
             or v_new.shape != ns or not (k_new.dtype is v_new.dtype is _BF16)
@@ -547,7 +553,7 @@ def specrouter_kv4_append(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_pow
                                        or v_seen.get_device() != here)
             or cache_mask is not None and _not_mask(cache_mask, B, L_cap, here)
             or shared_len is not None and _vector(shared_len, 1, _INT32, here)
-            or status is not None and status.get_device() != here):
+            or status is not None and _not_word(status, here)):
         _refuse(here, k_new=(k_new, None, (_BF16,), False), v_new=(v_new, ns, (_BF16,), False),
                 k_codes=(k_codes, (B, Hkv, L_cap, D // 2), (torch.uint8,), True),
                 k_powers=(k_powers, (B, Hkv, L_cap, D // 32), (torch.uint8,), True),
@@ -588,12 +594,12 @@ def specrouter_verify_attention_window(q, k_cache, v_cache, cache_mask, kv_len, 
     up to its own and the first `sinks`; out [B, gmax+1, Hq, D] fp32 or bf16."""
     here = _current()
     B, G1, Hq, D = qs = q.shape
-    cs = k_cache.shape
-    Hkv, L_cap = cs[1], cs[2]
+    Bk, Hkv, L_cap, Dk = cs = k_cache.shape
     out_bf16 = out.dtype is _BF16
     if (not (q.get_device() == k_cache.get_device() == v_cache.get_device() == kv_len.get_device()
              == gamma.get_device() == out.get_device() == here)
-            or len(cs) != 4 or cs[0] != B or cs[3] != D or v_cache.shape != cs or out.shape != qs
+            or Bk != B or Dk != D or v_cache.shape != cs or out.shape != qs or not -_INT_MAX <= window <= _INT_MAX
+            or not -_INT_MAX <= sinks <= _INT_MAX
             or not (q.dtype is k_cache.dtype is v_cache.dtype is _BF16)
             or not (out_bf16 or out.dtype is torch.float32)
             or not (q.is_contiguous() and k_cache.is_contiguous() and v_cache.is_contiguous() and out.is_contiguous()
@@ -601,7 +607,7 @@ def specrouter_verify_attention_window(q, k_cache, v_cache, cache_mask, kv_len, 
             or not (gamma.dtype is kv_len.dtype is _INT32) or gamma.numel() != B or kv_len.numel() != B
             or gamma.dim() != 1 or kv_len.dim() != 1
             or cache_mask is not None and _not_mask(cache_mask, B, L_cap, here)
-            or status is not None and status.get_device() != here):
+            or status is not None and _not_word(status, here)):
         _refuse(here, q=(q, None, (_BF16,), True), k_cache=(k_cache, (B, Hkv, L_cap, D), (_BF16,), True),
                 v_cache=(v_cache, (B, Hkv, L_cap, D), (_BF16,), True), cache_mask=(cache_mask, (B, L_cap), _BYTE, True),
                 kv_len=(kv_len, (B,), (_INT32,), True), gamma=(gamma, (B,), (_INT32,), True),
@@ -622,13 +628,14 @@ def specrouter_verify_attention_kv4(q, k_codes, k_powers, v_codes, v_powers, cac
     out [B, gmax+1, Hq, D] fp32 or bf16."""
     here = _current()
     B, G1, Hq, D = qs = q.shape
-    cs, ps = k_codes.shape, k_powers.shape
-    Hkv, L_cap = cs[1], cs[2]
+    _, Hkv, L_cap, _ = cs = k_codes.shape
+    ps = k_powers.shape
     out_bf16 = out.dtype is _BF16
     if (not (q.get_device() == k_codes.get_device() == k_powers.get_device() == v_codes.get_device()
              == v_powers.get_device() == kv_len.get_device() == gamma.get_device() == out.get_device() == here)
             or cs != (B, Hkv, L_cap, D // 2) or ps != (B, Hkv, L_cap, D // 32) or v_codes.shape != cs
-            or v_powers.shape != ps or out.shape != qs or q.dtype is not _BF16
+            or v_powers.shape != ps or out.shape != qs or q.dtype is not _BF16 or not -_INT_MAX <= window <= _INT_MAX
+            or not -_INT_MAX <= sinks <= _INT_MAX
             or not (k_codes.dtype is k_powers.dtype is v_codes.dtype is v_powers.dtype is torch.uint8)
             or not (out_bf16 or out.dtype is torch.float32)
             or not (q.is_contiguous() and k_codes.is_contiguous() and k_powers.is_contiguous()
@@ -637,7 +644,7 @@ def specrouter_verify_attention_kv4(q, k_codes, k_powers, v_codes, v_powers, cac
             or not (gamma.dtype is kv_len.dtype is _INT32) or gamma.numel() != B or kv_len.numel() != B
             or gamma.dim() != 1 or kv_len.dim() != 1
             or cache_mask is not None and _not_mask(cache_mask, B, L_cap, here)
-            or status is not None and status.get_device() != here):
+            or status is not None and _not_word(status, here)):
         _refuse(here, q=(q, None, (_BF16,), True), k_codes=(k_codes, (B, Hkv, L_cap, D // 2), (torch.uint8,), True),
                 k_powers=(k_powers, (B, Hkv, L_cap, D // 32), (torch.uint8,), True),
                 v_codes=(v_codes, (B, Hkv, L_cap, D // 2), (torch.uint8,), True),

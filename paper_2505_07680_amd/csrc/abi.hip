@@ -333,6 +333,7 @@ int specrouter_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
       !aligned16(q_weight) || !aligned16(k_weight))
     return SR_EINVAL;
   // in place only where input and output rows are the same rows
+  if (q_out == k_out || (q != k && (q_out == k || k_out == q))) return SR_EINVAL;
   if ((q_out == q && q_stride != (int64_t)Hq * D) || (k_out == k && k_stride != (int64_t)Hkv * D)) return SR_EINVAL;
   return sr::launch_qk_norm_rope(q, q_stride, k, k_stride, q_weight, k_weight, weight_dtype == SR_F32, eps, rope_table,
                                  max_positions, rot_dim, interleaved != 0, position, gamma, q_out, k_out, B, gamma_max,
@@ -352,6 +353,11 @@ int specrouter_kv4_append(const void* k_new, int64_t k_stride, const void* v_new
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_codes) || !aligned16(v_codes) || !aligned16(k_seen) ||
       !aligned16(v_seen) || ((uintptr_t)k_powers & 3u) != 0 || ((uintptr_t)v_powers & 3u) != 0)
     return SR_EINVAL;
+  // in place only where input and output rows are the same rows; the cursor is read while lengths are written
+  if (k_seen && ((k_seen == k_new && k_stride != (int64_t)Hkv * D) || k_seen == v_new || k_seen == v_seen))
+    return SR_EINVAL;
+  if (v_seen && ((v_seen == v_new && v_stride != (int64_t)Hkv * D) || v_seen == k_new)) return SR_EINVAL;
+  if (shared_len >= kv_len && shared_len < kv_len + B) return SR_EINVAL;
   return sr::launch_kv4_append(k_new, k_stride, v_new, v_stride, gamma, k_codes, k_powers, v_codes, v_powers,
                                cache_mask, kv_len, shared_len, k_seen, v_seen, B, gamma_max, Hkv, D, L_cap, status,
                                (hipStream_t)stream);

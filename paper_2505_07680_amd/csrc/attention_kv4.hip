@@ -203,7 +203,7 @@ attn_kv4_kernel(Kv4Args a) {
       st.kp[u] = __builtin_amdgcn_raw_buffer_load_b8(rkp, poff, pat, kPolicy);
       st.vp[u] = __builtin_amdgcn_raw_buffer_load_b8(rvp, poff, pat, kPolicy);
     }
-    st.mbyte = __builtin_amdgcn_raw_buffer_load_b8(rm, lane & (kTile - 1), kb0, 0);
+    st.mbyte = __builtin_amdgcn_raw_buffer_load_b8(rm, kb0 + (lane & (kTile - 1)), 0, 0);
   };
   // Tiles from key inner_lo to inner_hi are seen whole by every row (but for the mask).
   const int inner_lo = L - window, inner_hi = causal0 + 1 - kTile;

@@ -200,6 +200,7 @@ int launch_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, in
   }
   const int per = D == 64 ? prompt_rows<64>() : prompt_rows<128>();
   const int blocks = (int)((rows + per - 1) / per);
+  if ((long)B * blocks * kPromptThreads >= 1l << 32) return SR_EINVAL;  // (a launch's threads are counted in 32 bits)
   const Caching caching = caching_of((long)B * rows * D * 4 * (k_seen || v_seen ? 2 : 1));
   const auto kernel = caching == kPass ? prompt_kernel<kPass>(D)
                                        : caching == kReadOnce ? prompt_kernel<kReadOnce>(D) : prompt_kernel<kKeep>(D);

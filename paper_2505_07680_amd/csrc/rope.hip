@@ -166,6 +166,7 @@ int launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t 
   const int parts = (Hq + Hkv + per_wave - 1) / per_wave;
   const long n_items = (long)B * (gamma_max + 1) * parts;
   const long blocks = (n_items + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
+  if (blocks * kRopeThreads >= 1l << 32) return SR_EINVAL;  // (a launch's threads are counted in 32 bits)
   const Caching caching = caching_of((long)B * (gamma_max + 1) * (Hq + Hkv) * D * 4);
   const auto kernel = caching == kPass ? rope_kernel<kPass>(D, adjacent)
                                        : caching == kReadOnce ? rope_kernel<kReadOnce>(D, adjacent)

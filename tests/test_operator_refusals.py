@@ -5,11 +5,12 @@ import ctypes
 import os
 
 import pytest
+import torch
 
 from paper_2505_07680_amd import _lib
 
 no_device = pytest.mark.skipif(
-    __import__("torch").cuda.device_count() > 0, reason="host-only argument checks"
+    torch.cuda.device_count() > 0, reason="host-only argument checks"
 )
 EINVAL, EUNSUPPORTED, EWORKSPACE, ELAUNCH = _lib.SR_EINVAL, _lib.SR_EUNSUPPORTED, _lib.SR_EWORKSPACE, _lib.SR_ELAUNCH
 
@@ -94,3 +95,107 @@ def test_kv4_attention(lib):
     cases += [(18, s, EINVAL) for s in (0.0, float("nan"), float("inf"))]
     _refusals(lib.specrouter_verify_attention_kv4, good, cases)
     assert lib.specrouter_verify_attention_kv4_workspace_size(2, 4, 8, 3, 64, 512, 0, 0) == 0
+
+
+@no_device
+def test_rows_that_would_overwrite_each_other(lib):
+    """Outputs that are another argument, in place with wider rows, and a cursor among the lengths."""
+    Q, K = ctypes.c_void_p(8192), ctypes.c_void_p(16384)
+    good = [P, 512, Q, 128, None, None, 0, 1e-6, P, 100, 64, 0, P, P, P, Q, 2, 3, 8, 2, 64, None, None]
+    _refusals(lib.specrouter_qk_norm_rope, good, [(14, Q, EINVAL), (15, P, EINVAL), (15, K, ELAUNCH)])
+    lens = ctypes.c_void_p(65536)
+    good = [P, 128, Q, 128, P, P, P, P, P, None, lens, None, P, Q, 2, 3, 2, 64, 100, None, None]
+    cases = [(1, 256, EINVAL), (3, 256, EINVAL), (12, Q, EINVAL), (13, P, EINVAL), (11, lens, EINVAL),
+             (11, ctypes.c_void_p(65540), EINVAL), (11, ctypes.c_void_p(65544), ELAUNCH)]
+    _refusals(lib.specrouter_kv4_append, good, cases)
+    same = list(good)
+    same[12] = same[13] = K
+    assert lib.specrouter_kv4_append(*same) == EINVAL
+
+
+@no_device
+def test_more_threads_than_a_launch_counts(lib):
+    # 2^26 tokens of one query and one key head are 2^26 waves, 2^32 threads
+    good = [P, 64, P, 64, None, None, 0, 1e-6, P, 100, 64, 0, P, P, ctypes.c_void_p(8192), ctypes.c_void_p(16384),
+            1, (1 << 26) - 5, 1, 1, 64, None, None]
+    _refusals(lib.specrouter_qk_norm_rope, good, [(17, (1 << 26) - 1, EINVAL)])
+
+
+class _Shape:
+    """A tensor's outside: what a call checks before it takes any address."""
+
+    def __init__(self, *shape, dtype=torch.bfloat16, device=0):
+        self.shape, self.dtype, self.device = shape, dtype, device
+
+    get_device = lambda self: self.device
+    is_contiguous = lambda self: True
+    dim = lambda self: len(self.shape)
+    numel = lambda self: int(__import__("math").prod(self.shape))
+
+    def data_ptr(self):
+        raise AssertionError("the call went through")
+
+    def stride(self):
+        raise AssertionError("the call went through")
+
+
+I32, U8 = torch.int32, torch.uint8
+
+
+@pytest.fixture
+def device_0(monkeypatch):
+    monkeypatch.setattr(_lib, "_current", lambda: 0)
+
+
+def _rope_call(**change):
+    a = dict(q=_Shape(2, 3, 8, 64), k=_Shape(2, 3, 2, 64), q_weight=None, k_weight=None, eps=1e-6,
+             rope_table=_Shape(100, 64, dtype=torch.float32), position=_Shape(2, dtype=I32), gamma=_Shape(2, dtype=I32),
+             q_out=_Shape(2, 3, 8, 64), k_out=_Shape(2, 3, 2, 64))
+    _lib.specrouter_qk_norm_rope(**{**a, **change})
+
+
+def _append_call(**change):
+    codes, powers = _Shape(2, 2, 100, 32, dtype=U8), _Shape(2, 2, 100, 2, dtype=U8)
+    a = dict(k_new=_Shape(2, 3, 2, 64), v_new=_Shape(2, 3, 2, 64), gamma=_Shape(2, dtype=I32), k_codes=codes,
+             k_powers=powers, v_codes=codes, v_powers=powers, cache_mask=None, kv_len=_Shape(2, dtype=I32))
+    _lib.specrouter_kv4_append(**{**a, **change})
+
+
+def _window_call(**change):
+    a = dict(q=_Shape(2, 3, 8, 64), k_cache=_Shape(2, 2, 100, 64), v_cache=_Shape(2, 2, 100, 64), cache_mask=None,
+             kv_len=_Shape(2, dtype=I32), gamma=_Shape(2, dtype=I32), out=_Shape(2, 3, 8, 64), scale=0.125, window=16)
+    _lib.specrouter_verify_attention_window(**{**a, **change})
+
+
+def _kv4_call(**change):
+    codes, powers = _Shape(2, 2, 100, 32, dtype=U8), _Shape(2, 2, 100, 2, dtype=U8)
+    a = dict(q=_Shape(2, 3, 8, 64), k_codes=codes, k_powers=powers, v_codes=codes, v_powers=powers, cache_mask=None,
+             kv_len=_Shape(2, dtype=I32), gamma=_Shape(2, dtype=I32), out=_Shape(2, 3, 8, 64), scale=0.125)
+    _lib.specrouter_verify_attention_kv4(**{**a, **change})
+
+
+WRONG_STATUS = (dict(status=_Shape(1, dtype=torch.int64)), dict(status=_Shape(1, dtype=I32, device=1)))
+
+
+@pytest.mark.parametrize("call, changes", [
+    (_rope_call, [dict(k_weight=_Shape(64, dtype=torch.float64)), dict(q_weight=_Shape(64, dtype=torch.float64)),
+                  dict(q_weight=_Shape(64), k_weight=_Shape(64, dtype=torch.float32)),
+                  dict(k=_Shape(2, 3, 64)), dict(k=_Shape(2, 4, 2, 64)), dict(k_out=_Shape(2, 3, 8, 64)),
+                  dict(position=_Shape(2, 1, dtype=I32)), dict(gamma=_Shape(3, dtype=I32)),
+                  dict(rope_table=_Shape(1 << 31, 64, dtype=torch.float32))]),
+    (_append_call, [dict(k_codes=_Shape(2, 100, 32, dtype=U8)), dict(v_codes=_Shape(2, 2, 99, 32, dtype=U8)),
+                    dict(k_powers=_Shape(2, 2, 100, 1, dtype=U8)), dict(kv_len=_Shape(2, dtype=torch.int64)),
+                    dict(k_seen=_Shape(2, 3, 2, 128)), dict(shared_len=_Shape(2, dtype=I32))]),
+    (_window_call, [dict(window=2 ** 32 + 5), dict(window=-2 ** 32 + 5), dict(sinks=2 ** 32), dict(k_cache=_Shape(2, 2, 64)),
+                    dict(v_cache=_Shape(2, 2, 99, 64)), dict(out=_Shape(2, 3, 8, 64, dtype=torch.float16)),
+                    dict(kv_len=_Shape(1, dtype=I32))]),
+    (_kv4_call, [dict(window=2 ** 32 + 5), dict(sinks=2 ** 32), dict(k_codes=_Shape(2, 100, 32, dtype=U8)),
+                 dict(v_powers=_Shape(2, 2, 100, 1, dtype=U8)), dict(q=_Shape(2, 3, 8, 64, dtype=torch.float16)),
+                 dict(cache_mask=_Shape(2, 99, dtype=U8))]),
+])
+def test_bindings_refuse_before_they_take_an_address(lib, device_0, call, changes):
+    with pytest.raises(AssertionError, match="went through"):
+        call()
+    for change in (*changes, *WRONG_STATUS):
+        with pytest.raises((ValueError, TypeError)):
+            call(**change)
