@@ -141,9 +141,9 @@ int specrouter_verify_attention(const void* q, const void* k_cache, const void* 
  * j < sinks. Positions are cache rows, masked ones counted. Only the rows that
  * some new row can see are read: at most window + gamma_b + sinks per sequence
  * and kv head, and what lies between the sinks and the window is ignored
- * whatever it holds. NaN or infinity among a row's own keys and values gives NaN
- * in that row; in V of a key that some new row sees it may give NaN in the
- * sequence's other rows too, as 0 times it is NaN.
+ * whatever it holds. NaN in a key that a row sees gives NaN in that row; NaN or
+ * infinity in V of such a key gives NaN or infinity in its column there, and may
+ * give NaN in the sequence's other rows too, as 0 times it is NaN.
  *
  * window     >= 1 (from L_cap on it hides nothing); sinks >= 0; else SR_EINVAL
  * out        [B][gamma_max+1][Hq][D] of out_dtype: SR_F32, or SR_BF16 (the same

@@ -309,7 +309,9 @@ __device__ __forceinline__ void merge_and_store(unsigned char* lds, const floatx
     }
     return;
   }
-  // (m, l) of every split: four threads per row take the splits in turn
+  // (m, l) of every split: four threads per row take the splits in turn. A split
+  // whose scores were all NaN has reference -inf and sum NaN, which NANS passes on.
+  constexpr float kNone = NANS ? 1.f : 0.f;
   for (int row = tid / 4; row < n_rows; row += kT / 4) {
     constexpr int kMl = 8;
     float M = kNegInf, den = 0.f;
@@ -323,12 +325,12 @@ __device__ __forceinline__ void merge_and_store(unsigned char* lds, const floatx
       float Mn = M;
 #pragma unroll
       for (int j = 0; j < kMl; ++j) Mn = sp0 + 4 * j < ns ? fmaxf(Mn, x[j].x) : Mn;
-      den = Mn == kNegInf ? 0.f : den * exp2_hw(M - Mn);
+      den = Mn == kNegInf ? den * kNone : den * exp2_hw(M - Mn);
 #pragma unroll
       for (int j = 0; j < kMl; ++j) {
         const int sp = sp0 + 4 * j;
         if (sp < ns) {
-          if (Mn != kNegInf) den += x[j].y * exp2_hw(x[j].x - Mn);
+          if (NANS || Mn != kNegInf) den += x[j].y * (Mn == kNegInf ? 1.f : exp2_hw(x[j].x - Mn));
           if (sp < kMlBlock) mS[sp * kRows + row] = x[j].x;
         }
       }
@@ -341,7 +343,7 @@ __device__ __forceinline__ void merge_and_store(unsigned char* lds, const floatx
       const float Do = d == 1 ? perm_f32<dpp::kXor1>(den) : perm_f32<dpp::kXor2>(den);
       const float Mn = fmaxf(M, Mo);
       // (the fused operand is written out, so that every kernel rounds alike)
-      den = Mn == kNegInf ? 0.f : fmaf(den, exp2_hw(M - Mn), Do * exp2_hw(Mo - Mn));
+      den = Mn == kNegInf ? (den + Do) * kNone : fmaf(den, exp2_hw(M - Mn), Do * exp2_hw(Mo - Mn));
       M = Mn;
     }
     if (tid % 4 == 0) {

@@ -304,3 +304,28 @@ def test_binding_refuses_what_does_not_fit(kind):
             x.call(kind, 64, 0, good, ws)
         setattr(x, name, keep)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_nan_keys_reach_the_output_through_every_merge(kind, D):
+    """A sequence split many ways: rows whose only visible keys are NaN, or some of whose
+    splits hold nothing but a NaN key, are NaN; a row that sees no key stays 0."""
+    rng = np.random.default_rng(15)
+    cap = 20000
+    x = Inputs(rng, 1, 2, 4, 2, D, cap, [19000], holes=0.0)
+    for at, nan in (([700], [700]), ([700, 15000], [700]), ([700, 701, 9000, 18999], [700, 9000]), (range(0, 19000, 37), [37])):
+        x.mask[:] = 0
+        x.mask[0, list(at)] = 1
+        k, p = x.k.copy(), x.cache4[1].copy()
+        x.k[0, 0, nan] = 0x7FC0
+        x.cache4[1][0, 0, nan] = 255
+        out = host(x.run(kind, cap, 0, dtype=torch.float32)[0])
+        x.k, x.cache4[1] = k, p
+        say(f"{kind} D={D} visible {len(list(at))}")
+        assert np.isnan(out[0, :, :2]).all()
+        assert np.isfinite(out[0, :, 2:]).all() and (out[0, :, 2:] != 0).any()
+    x.mask[:] = 0
+    x.k[0, 0] = 0x7FC0
+    x.cache4[1][0, 0] = 255
+    assert (host(x.run(kind, cap, 0, dtype=torch.float32)[0]) == 0).all()
