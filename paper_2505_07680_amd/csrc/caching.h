@@ -6,7 +6,7 @@
 // to be dropped first, so that they do not drive the outputs out (kReadOnce);
 // and beyond what the memory-side cache keeps for the reader as well, the outputs are
 // marked too (kPass). Normalised and rotated heads, alone / followed by a
-// copy of the result, us:
+// copy of the result, us (four steps a wave):
 //    16 MB   keep  7.4 / 12.5   read once  7.7 / 12.9   pass  6.2 / 13.0
 //    42 MB        12.3 / 23.2             12.4 / 20.8         9.8 / 21.3
 //    86 MB        24.0 / 39.6             21.5 / 36.6        19.8 / 40.6
@@ -24,7 +24,7 @@ namespace sr {
 
 enum Caching { kKeep, kReadOnce, kPass };
 
-// of a call that moves this many bytes in and out
+// of a call that moves at most this many bytes in and out
 inline Caching caching_of(long bytes) {
   return bytes < (36l << 20) ? kKeep : bytes < (128l << 20) ? kReadOnce : kPass;
 }

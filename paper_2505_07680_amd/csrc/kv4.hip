@@ -8,12 +8,17 @@
 // power is exact (both bf16), so the codes are a function of the row alone. A
 // group that holds an infinity or a NaN gets p = 255, which reads as NaN.
 //
-// Bound by HBM for prompts, by latency for a step's few rows. Four lanes take a
-// group of 32 (a 16-byte load of eight bf16 each; the group's largest magnitude
-// is an integer maximum over the four); the conversion is the hardware's
-// (v_cvt_scalef32_pk_fp4_bf16 divides by the power of two and rounds to
+// Four lanes take a group of 32 (a 16-byte load of eight bf16 each; the group's
+// largest magnitude is an integer maximum over the four); the conversion is the
+// hardware's (v_cvt_scalef32_pk_fp4_bf16 divides by the power of two and rounds to
 // nearest even). A wave takes consecutive positions of one head, so that its
 // stores are one run of the head's slab.
+//
+// Prompts are bound by HBM and their many short runs (8 KB to 2 KB apart in what is
+// read, 16 bytes a row's powers): 8 of 2048 to 4095 rows, 8 heads of 128, with
+// the values that attention will see, 228 MB, 40 us in the rows' kernel (5.7 TB/s)
+// and 4 in the lengths'. A step's rows are bound by latency: 5.2 us for 256
+// sequences (13 MB), of which the launch is about half.
 
 #include "caching.h"
 

@@ -8,13 +8,16 @@
 // over the pairs (a, b) of the rotated part, t the pair's angle at the row's
 // position, from a table. Everything in 32 bits, rounded to bf16 once.
 //
-// Bound by HBM for prompts (each value is read and written once) and by the
-// launch for single tokens. A head takes D/8 lanes of eight values each (one
-// 16-byte load and store), so a wave holds 4 heads of 128 or 8 of 64 at a time,
-// all of one token: the angles are loaded once and stay in registers for the
-// wave's kHeadSteps steps, whose loads are all in flight before the first is
-// used. With pairs half a rotation apart the partner's values come from the
-// lane that holds them, by way of the LDS crossbar.
+// A head takes D/8 lanes of eight values each (one 16-byte load and store), so a
+// wave holds 4 heads of 128 or 8 of 64 at a time, all of one token: the angles are
+// loaded once and stay in registers for the wave's few steps, whose loads are all
+// in flight before the first is used. With pairs half a rotation apart the
+// partner's values come from the lane that holds them, by way of the LDS crossbar.
+//
+// Bound by HBM for prompts: 4 of 8100 rows, 72 heads of 128, 190 us, 6.3 TB/s read
+// and written (a large device copy reaches 4.9). 256 sequences' steps (30 MB)
+// take 9.7 us, 3.1 TB/s: the launch, the cold caches and one wave's chain of
+// position, loads, angles and store. One token takes 2.4 us, the launch.
 
 #include "caching.h"
 
@@ -22,7 +25,12 @@ namespace sr {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kHeadSteps = 4;
+// Steps of a wave. While the data comes from or stays in a cache, twice the waves
+// hide more than a longer wave's loads and the reuse of its angles save (40 heads
+// of 128, us with two and with four steps: one token 2.4 and 2.7, 192 tokens 3.4
+// and 4.2, 1443 tokens 9.7 and 11.1, 4096 tokens 20.7 and 21.5);
+// streamed from HBM it is the other way round (333 MB 64 and 58, 1.2 GB 195 and 190).
+constexpr int head_steps(int caching) { return caching == kPass ? 4 : 2; }
 
 __device__ __forceinline__ float lane_f32(float x, int src_lane) {
   return __int_as_float(__builtin_amdgcn_ds_bpermute(src_lane * 4, __float_as_int(x)));
@@ -60,6 +68,7 @@ qk_norm_rope_kernel(const uint16_t* q, int64_t q_stride, const uint16_t* k, int6
                     uint16_t* k_out, int gmax, int Hq, int Hkv, int parts, uint32_t n_items, int32_t* __restrict__ status) {
   constexpr int kLanes = D / 8;        // lanes per head
   constexpr int kHeads = 64 / kLanes;  // heads per step of a wave
+  constexpr int kHeadSteps = head_steps(CACHING);
   // item: (token, part of its heads)
   const uint32_t item = blockIdx.x * (kRopeThreads / 64) + (uint32_t)wave_id();
   if (item >= n_items) return;
@@ -162,12 +171,12 @@ int launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t 
                         const void* k_weight, bool w_f32, float eps, const float* table, int max_positions, int rot,
                         bool adjacent, const int32_t* position, const int32_t* gamma, void* q_out, void* k_out, int B,
                         int gamma_max, int Hq, int Hkv, int D, int32_t* status, hipStream_t stream) {
-  const int per_wave = 64 / (D / 8) * kHeadSteps;
+  const Caching caching = caching_of((long)B * (gamma_max + 1) * (Hq + Hkv) * D * 4);
+  const int per_wave = 64 / (D / 8) * head_steps(caching);
   const int parts = (Hq + Hkv + per_wave - 1) / per_wave;
   const long n_items = (long)B * (gamma_max + 1) * parts;
   const long blocks = (n_items + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
   if (blocks * kRopeThreads >= 1l << 32) return SR_EINVAL;  // (a launch's threads are counted in 32 bits)
-  const Caching caching = caching_of((long)B * (gamma_max + 1) * (Hq + Hkv) * D * 4);
   const auto kernel = caching == kPass ? rope_kernel<kPass>(D, adjacent)
                                        : caching == kReadOnce ? rope_kernel<kReadOnce>(D, adjacent)
                                                               : rope_kernel<kKeep>(D, adjacent);
