@@ -520,10 +520,11 @@ def specrouter_qk_norm_rope(q, k, q_weight, k_weight, eps, rope_table, position,
                 rope_table=(rope_table, None, (torch.float32,), True),
                 q_weight=(q_weight, (D,), _OUT, True),
                 k_weight=(k_weight, (D,), _OUT if q_weight is None else (w.dtype,), True), status=(status, None, (_INT32,), True))
-    rc = load().specrouter_qk_norm_rope(
+    rc = (_lib or load()).specrouter_qk_norm_rope(
         q.data_ptr(), _row_stride(q, rows, Hq, D, "q"), k.data_ptr(), _row_stride(k, rows, Hkv, D, "k"), _ptr(q_weight), _ptr(k_weight), code,
         eps, rope_table.data_ptr(), max_positions, rot, 1 if interleaved else 0, position.data_ptr(), gamma.data_ptr(),
-        q_out.data_ptr(), k_out.data_ptr(), B, rows - 1, Hq, Hkv, D, _ptr(status), _stream())
+        q_out.data_ptr(), k_out.data_ptr(), B, rows - 1, Hq, Hkv, D, _ptr(status),
+        torch._C._cuda_getCurrentRawStream(here))
     if rc:
         _check(rc, "specrouter_qk_norm_rope")
 
@@ -563,11 +564,11 @@ def specrouter_kv4_append(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_pow
                 kv_len=(kv_len, (B,), (_INT32,), True), shared_len=(shared_len, (1,), (_INT32,), True),
                 k_seen=(k_seen, ns, (_BF16,), True), v_seen=(v_seen, ns, (_BF16,), True),
                 status=(status, None, (_INT32,), True))
-    rc = load().specrouter_kv4_append(
+    rc = (_lib or load()).specrouter_kv4_append(
         k_new.data_ptr(), _row_stride(k_new, rows, Hkv, D, "k_new"), v_new.data_ptr(), _row_stride(v_new, rows, Hkv, D, "v_new"), gamma.data_ptr(),
         k_codes.data_ptr(), k_powers.data_ptr(), v_codes.data_ptr(), v_powers.data_ptr(), _ptr(cache_mask),
         kv_len.data_ptr(), _ptr(shared_len), _ptr(k_seen), _ptr(v_seen), B, rows - 1, Hkv, D, L_cap, _ptr(status),
-        _stream())
+        torch._C._cuda_getCurrentRawStream(here))
     if rc:
         _check(rc, "specrouter_kv4_append")
 
@@ -612,10 +613,10 @@ def specrouter_verify_attention_window(q, k_cache, v_cache, cache_mask, kv_len, 
                 v_cache=(v_cache, (B, Hkv, L_cap, D), (_BF16,), True), cache_mask=(cache_mask, (B, L_cap), _BYTE, True),
                 kv_len=(kv_len, (B,), (_INT32,), True), gamma=(gamma, (B,), (_INT32,), True),
                 out=(out, qs, _OUT, True), status=(status, None, (_INT32,), True))
-    rc = load().specrouter_verify_attention_window(
+    rc = (_lib or load()).specrouter_verify_attention_window(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(cache_mask), kv_len.data_ptr(), gamma.data_ptr(),
         out.data_ptr(), SR_BF16 if out_bf16 else SR_F32, B, G1 - 1, Hq, Hkv, D, L_cap, window, sinks, scale,
-        _ptr(workspace), _bytes_of(workspace, here), _ptr(status), _stream())
+        _ptr(workspace), _bytes_of(workspace, here), _ptr(status), torch._C._cuda_getCurrentRawStream(here))
     if rc:
         _check(rc, "specrouter_verify_attention_window")
     return out
@@ -651,11 +652,11 @@ def specrouter_verify_attention_kv4(q, k_codes, k_powers, v_codes, v_powers, cac
                 v_powers=(v_powers, (B, Hkv, L_cap, D // 32), (torch.uint8,), True),
                 cache_mask=(cache_mask, (B, L_cap), _BYTE, True), kv_len=(kv_len, (B,), (_INT32,), True),
                 gamma=(gamma, (B,), (_INT32,), True), out=(out, qs, _OUT, True), status=(status, None, (_INT32,), True))
-    rc = load().specrouter_verify_attention_kv4(
+    rc = (_lib or load()).specrouter_verify_attention_kv4(
         q.data_ptr(), k_codes.data_ptr(), k_powers.data_ptr(), v_codes.data_ptr(), v_powers.data_ptr(),
         _ptr(cache_mask), kv_len.data_ptr(), gamma.data_ptr(), out.data_ptr(), SR_BF16 if out_bf16 else SR_F32, B,
         G1 - 1, Hq, Hkv, D, L_cap, window, sinks, scale, _ptr(workspace), _bytes_of(workspace, here), _ptr(status),
-        _stream())
+        torch._C._cuda_getCurrentRawStream(here))
     if rc:
         _check(rc, "specrouter_verify_attention_kv4")
     return out
