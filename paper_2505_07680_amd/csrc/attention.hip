@@ -111,6 +111,23 @@ int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_rows,
   plan->q_chunks = (R + rows_per_chunk - 1) / rows_per_chunk;
   const int cus = device_cu_count();
   if (cus <= 0) return SR_ELAUNCH;
+  // With a window, more than 48 rows go to chunks of up to 48, four waves each, which
+  // read the same keys through an L2 but fit two to a CU and waste fewer row
+  // blocks; two groups in eight waves stay where they leave no CU idle, save no rows
+  // and stream long. (64 query heads on 8 of 128, us in eight waves and in chunks: one sequence
+  // of 1024 positions, 64 rows, 20.0 and 13.6; 16 of 1024 28.8 and 23.4, of 3000
+  // 45.5 and 53.7; 32 of 512 25.2 and 24.3, of 640 26.6 and 29.9; 40 of 2048,
+  // 72 rows, 118 and 98, 136 rows 164 and 120; 256 of 512, 72 rows, 217 and 176.)
+  if (window > 0 && plan->qg > 1) {
+    const int chunks = (R + 16 * kMaxNQ - 1) / (16 * kMaxNQ);
+    const long jobs = (long)B * Hkv * plan->q_chunks;
+    const bool even = jobs <= cus && cus % jobs == 0;
+    if (!even || chunks < kMaxQG * plan->q_chunks || jobs * L_cap <= 600l * cus) {
+      plan->qg = 1;
+      plan->q_chunks = chunks;
+      plan->nq = ((R + chunks - 1) / chunks + 15) / 16;
+    }
+  }
   const int threads = plan->qg == 1 ? Shape<1>::kThreads : Shape<kMaxQG>::kThreads;
   const int per_cu = resident_per_cu((const void*)(window > 0 ? window_kernel(D, plan->nq, plan->qg, plan->q_chunks)
                                                                  : pick_split(D, plan->nq, plan->qg, plan->q_chunks, false)), threads, 0);
@@ -189,7 +206,13 @@ int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_rows,
   plan->part_offset = counters;
   size_t bytes = plan->n_splits > 1 ? counters + (size_t)B * Hkv * plan->n_splits * R * (D + 2) * sizeof(float) : 0;
   const long n_jobs = (long)plan->n_splits * pairs;
-  plan->ordered = n_jobs > target ? 1 : 0;
+  // (With a window, sequences differ by its length at most. Up to 128 keys the order
+  // kernel's 5 us are more than that: 251 sequences of 22 positions 15.1 us with it, 11.6
+  // without; so they are for a few chunks more than fit at once: 33 sequences of 512
+  // positions, 72 rows, 42 and 36.)
+  const bool alike = window > 0 && (L_cap <= 2 * kTileKeys ||
+                                    (plan->q_chunks > 1 && L_cap <= 704 && 2 * n_jobs <= 3 * target));
+  plan->ordered = n_jobs > target && !alike ? 1 : 0;
   plan->order_offset = (bytes + 15) / 16 * 16;
   if (plan->ordered) bytes = plan->order_offset + (size_t)n_jobs * sizeof(int32_t);
   plan->workspace_bytes = bytes;

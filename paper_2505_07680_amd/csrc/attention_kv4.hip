@@ -443,11 +443,16 @@ int attention_kv4_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_r
   // with 24, 31 with 48; 24 sequences of 256 to 8192 keys 65 with 1, 41 with 3 or 4, 50
   // with 10; 16 sequences of 2048 24 with 1, 20 with 2 to 4, 33 with 8.)
   constexpr long kPerSplit = 64;
+  // A window shorter than the cache makes the sequences alike, so that nothing
+  // balances a second turn of workgroups (46 sequences of 1648 positions, 4/1 heads by 8,
+  // gamma 4: 34 us with one split, 45 with two).
+  const bool alike = L < cache_rows;
   const long most = (2L * cus + pairs - 1) / pairs;
   long splits = 1, best = 0;
   for (long n = 1; n <= most; ++n) {
-    const long keys = (L + n - 1) / n;
-    const long t = (pairs * n > 2L * cus ? keys * pairs * n / (2L * cus) : keys) + (n > 1 ? n * kPerSplit : 0);
+    const long keys = (L + n - 1) / n, jobs = pairs * n;
+    const long t = (jobs <= 2L * cus ? keys : alike ? (jobs + 2L * cus - 1) / (2L * cus) * keys : keys * jobs / (2L * cus)) +
+                   (n > 1 ? n * kPerSplit : 0);
     if (n == 1 || t < best) best = t, splits = n;
   }
   const long max_splits = (L + kTile - 1) / kTile;
@@ -474,7 +479,9 @@ int attention_kv4_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_r
   const size_t counters = (size_t)pairs * kCounterStride * sizeof(uint32_t);
   plan->part_offset = counters;
   size_t bytes = plan->n_splits > 1 ? counters + (size_t)B * Hkv * plan->n_splits * R * (D + 2) * sizeof(float) : 0;
-  plan->ordered = n_jobs > target ? 1 : 0;
+  // (Up to 1024 keys what it balances is less than the order kernel's 5 us: 256
+  // sequences of 100 to 300 keys 36.6 us with it, 34.1 without, of 100 to 700 45.3 and 43.6.)
+  plan->ordered = n_jobs > target && L > 1024 ? 1 : 0;
   plan->order_offset = (bytes + 15) / 16 * 16;
   if (plan->ordered) bytes = plan->order_offset + (size_t)n_jobs * sizeof(int32_t);
   plan->workspace_bytes = bytes;

@@ -53,7 +53,8 @@
 // putting -infinity in the scores' place, and with one query group leaves row
 // blocks without live rows out of the products too (the loop is compiled for
 // each number of them): 64 sequences of 1024 positions, gamma 1 to 8, 58 -> 53 us,
-// 16 of 4096 with 72 rows 75 -> 67. The kernel without a window is compiled apart
+// 16 of 4096 with 72 rows 75 -> 67. More than 48 rows mostly go to chunks of four waves
+// instead of eight waves (see attention_plan). The kernel without a window is compiled apart
 // and keeps its own arithmetic.
 
 #pragma once
@@ -690,8 +691,10 @@ SplitKernel pick_split(int nq, int qg, int q_chunks) {
   if (qg == 1) {
     switch (nq) {
       case 1: return attn_split_kernel<D, 1, 1, true, FOLLOW, WIN>;
-      case 2: return attn_split_kernel<D, 2, 1, true, FOLLOW, WIN>;
-      default: return attn_split_kernel<D, 3, 1, true, FOLLOW, WIN>;
+      case 2: return !WIN || q_chunks == 1 ? attn_split_kernel<D, 2, 1, true, FOLLOW, WIN>
+                                           : attn_split_kernel<D, 2, 1, !WIN, FOLLOW, WIN>;
+      default: return !WIN || q_chunks == 1 ? attn_split_kernel<D, 3, 1, true, FOLLOW, WIN>
+                                            : attn_split_kernel<D, 3, 1, !WIN, FOLLOW, WIN>;
     }
   }
   if (nq == 2) return attn_split_kernel<D, 2, 2, true, FOLLOW, WIN>;

@@ -329,3 +329,22 @@ def test_nan_keys_reach_the_output_through_every_merge(kind, D):
     x.k[0, 0] = 0x7FC0
     x.cache4[1][0, 0] = 255
     assert (host(x.run(kind, cap, 0, dtype=torch.float32)[0]) == 0).all()
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,G1,cap,win", [
+    (2, 64, 8, 128, 8, 10000, 9600),  # two groups of two row blocks
+    (2, 64, 8, 64, 9, 10000, 9600),   # of three
+    (1, 24, 2, 128, 16, 40000, 39000),  # two chunks of them
+    (1, 24, 2, 64, 16, 40000, 39000),
+    (40, 64, 8, 64, 9, 700, 300),     # chunks of two row blocks, in order
+    (33, 64, 8, 64, 12, 700, 600),    # of three, not ordered
+    (3, 32, 1, 64, 10, 500, 300),     # seven chunks
+])
+def test_forms_of_many_rows(B, Hq, Hkv, D, G1, cap, win):
+    rng = np.random.default_rng(16)
+    ctx = rng.integers(cap - cap // 4, cap - G1, B)
+    gamma = rng.integers(0, G1, B).astype(np.int32)
+    gamma[0] = G1 - 1
+    x = Inputs(rng, B, G1, Hq, Hkv, D, cap, ctx, gamma=gamma, holes=0.05, four=False)
+    say(f"B={B} rows={Hq // Hkv * G1} D={D} window={win}")
+    x.compare("window", win, 5)
