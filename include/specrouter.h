@@ -455,7 +455,9 @@ int specrouter_kv4_append(const void* k_new, int64_t k_stride, const void* v_new
  * no new row sees are ignored whatever they hold (NaN in V that one row sees: as
  * for the window call). out_dtype as for the window
  * call; workspace of specrouter_verify_attention_kv4_workspace_size() bytes for
- * the same arguments, zero-filled before its first use.
+ * the same arguments, zero-filled before its first use. Repeated calls give
+ * identical bits; where a sequence's keys are split, and so its last bits, may
+ * depend on the lengths of the others in its batch.
  */
 size_t specrouter_verify_attention_kv4_workspace_size(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap,
                                                       int window, int sinks);

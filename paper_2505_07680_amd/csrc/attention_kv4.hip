@@ -3,8 +3,8 @@
 // without a window, over e2m1 codes with a power of two per 32 elements of a row.
 //
 // Work decomposition as over a bf16 cache: a workgroup of four waves takes one
-// (sequence, kv head, query chunk, key split), the waves deal the split's tiles
-// of 32 keys among themselves, and their states merge through LDS, those of
+// (sequence, kv head, query chunk, key split; small batches split by their lengths,
+// see deal), the waves deal the split's tiles of 32 keys among themselves, and their states merge through LDS, those of
 // several splits through the workspace.
 //
 // A code times its power is exact in bf16, so both products run on bf16 MFMA and
@@ -91,9 +91,83 @@ struct Kv4Args {
   const int32_t* order;
   int B, gmax, Hq, Hkv, L_cap, window, sinks;
   float scale_log2;
-  int split_keys, n_splits, q_chunks;
+  int split_keys, n_splits, q_chunks, units;
   int32_t* status;
 };
+
+// Of 32-bit lane values: their sum and maximum over the wave, and the sums up to each lane.
+__device__ __forceinline__ int over_rows(int x, int row) { return __builtin_amdgcn_readlane(x, row * 16); }
+__device__ __forceinline__ int wave_sum_i(int x) {
+  x += (int)perm_u32<dpp::kXor1>((uint32_t)x);
+  x += (int)perm_u32<dpp::kXor2>((uint32_t)x);
+  x += (int)perm_u32<dpp::kHalfMirror>((uint32_t)x);
+  x += (int)perm_u32<dpp::kMirror>((uint32_t)x);
+  return over_rows(x, 0) + over_rows(x, 1) + over_rows(x, 2) + over_rows(x, 3);
+}
+__device__ __forceinline__ int wave_max_i(int x) {
+  x = max(x, (int)perm_u32<dpp::kXor1>((uint32_t)x));
+  x = max(x, (int)perm_u32<dpp::kXor2>((uint32_t)x));
+  x = max(x, (int)perm_u32<dpp::kHalfMirror>((uint32_t)x));
+  x = max(x, (int)perm_u32<dpp::kMirror>((uint32_t)x));
+  return max(max(over_rows(x, 0), over_rows(x, 1)), max(over_rows(x, 2), over_rows(x, 3)));
+}
+template <int N>
+__device__ __forceinline__ int row_shr(int x) {  // lane i: lane i - N of its row of 16, or 0
+  return __builtin_amdgcn_update_dpp(0, x, 0x110 + N, 0xf, 0xf, true);
+}
+__device__ __forceinline__ int wave_scan_i(int x) {
+  x += row_shr<1>(x);
+  x += row_shr<2>(x);
+  x += row_shr<4>(x);
+  x += row_shr<8>(x);
+  const int r0 = __builtin_amdgcn_readlane(x, 15), r1 = __builtin_amdgcn_readlane(x, 31);
+  const int r2 = __builtin_amdgcn_readlane(x, 47), row = (int)(threadIdx.x & 63) / 16;
+  return x + (row > 0 ? r0 : 0) + (row > 1 ? r1 : 0) + (row > 2 ? r2 : 0);
+}
+
+// The work of a launch dealt by the lengths (up to 64 sequences, one per lane):
+// splits of one size for all, the least that gives no more (sequence, split) pairs
+// than there is room for, but not below what a merge costs (a split of K keys and
+// its share of the merge take K + 64 L / K, least at K = sqrt(64 L)). Unit s of
+// the launch is split s - first of sequence b; every wave finds the same.
+constexpr int kMaxDealt = 64;
+constexpr int kMergeKeys = 64;  // keys that a merged split's time is worth
+struct Dealt {
+  int b, first, tiles;  // sequence, its first unit, tiles per split
+  bool any;
+  int gam, L;
+};
+inline __host__ __device__ int least_tiles(int tiles) {
+  return tiles * kTile <= 4 * kMergeKeys ? tiles : (int)ceilf(sqrtf((float)tiles * ((float)kMergeKeys / kTile)));
+}
+__device__ __forceinline__ Dealt deal(const Kv4Args& a, int window, int s) {
+  const int lane = threadIdx.x & 63;
+  const int lb = min(lane, a.B - 1);
+  const int gam = a.gamma[lb], L = a.kv_len[lb];
+  const bool valid = gam >= 0 && gam <= a.gmax && L >= gam + 1 && L <= a.L_cap;
+  const Reach<kTile> reach(valid ? L - gam - 1 : 0, valid ? L : 0, window, a.sinks);
+  const int tiles = lane < a.B ? max(reach.tiles, 1) : 0;  // (bad data: one split, which writes zeros)
+  const int most = wave_max_i(tiles), total = wave_sum_i(tiles);
+  auto splits = [&](int size) __attribute__((always_inline)) { return (int)((uint32_t)(tiles + size - 1) / (uint32_t)size); };
+  int lo = min(max(least_tiles(most), (total + a.units - 1) / a.units), most), hi = most;  // (hi: one split each)
+  if (wave_sum_i(splits(lo)) <= a.units) {
+    hi = lo;
+  } else {
+    const int room = a.units - a.B;  // sum ceil(t / size) < total / size + B
+    if (room > 0) hi = min(hi, (total + room - 1) / room);
+    while (hi - lo > 1 + lo / 32) {
+      const int mid = (lo + hi) / 2;
+      if (wave_sum_i(splits(mid)) <= a.units) hi = mid;
+      else lo = mid;
+    }
+  }
+  const int n = splits(hi), upto = wave_scan_i(n);
+  const int b = __builtin_popcountll(__ballot(upto <= s));
+  const bool any = b < a.B;
+  const int bs = any ? b : 0;
+  return {bs, __builtin_amdgcn_readlane(upto - n, bs), hi, any, __builtin_amdgcn_readlane(gam, bs),
+          __builtin_amdgcn_readlane(L, bs)};
+}
 
 // RING: tiles in flight per wave (see attention_kv4_plan). With one and two row
 // blocks, 168 registers, three waves fit a SIMD; what is kept in scratch there is the
@@ -110,20 +184,35 @@ attn_kv4_kernel(Kv4Args a) {
   __shared__ __attribute__((aligned(16))) unsigned char lds[LL::kBytes];
 
   const int P = a.B * a.Hkv;
-  const int rest = (int)(blockIdx.x / (unsigned)P);
-  const int code = a.order ? __builtin_amdgcn_readfirstlane(a.order[blockIdx.x])
-                           : ((int)(blockIdx.x % (unsigned)P) * a.q_chunks + rest / a.n_splits) * a.n_splits +
-                                 (a.n_splits - 1 - rest % a.n_splits);
-  const int split = code % a.n_splits;
-  const int job = code / a.n_splits;
-  const int qc = job % a.q_chunks;
-  const int pair_id = job / a.q_chunks;
-  const int g = pair_id % a.Hkv;
-  const int b = pair_id / a.Hkv;
+  const int window = a.window > 0 ? a.window : 0x7fffffff;
+  const int sinks = a.sinks;
+  int split, qc, g, b, gam, L, tiles_per = a.split_keys / kTile, n_splits = a.n_splits, pairs = P;
+  size_t pair;  // with the splits of one, the record block of a split's partial: (pair n_splits + split)
+  if (a.units > 0) {  // heads fastest, then units, then query chunks
+    const int rest = (int)(blockIdx.x / (unsigned)a.Hkv);
+    const Dealt d = deal(a, window, rest % a.units);
+    if (!d.any) return;  // (the whole workgroup)
+    g = (int)(blockIdx.x % (unsigned)a.Hkv);
+    qc = rest / a.units;
+    b = d.b, split = rest % a.units - d.first, gam = d.gam, L = d.L, tiles_per = d.tiles;
+    n_splits = 1, pairs = a.Hkv * a.units, pair = (size_t)(g * a.units + d.first);
+  } else {
+    const int rest = (int)(blockIdx.x / (unsigned)P);
+    const int code = a.order ? __builtin_amdgcn_readfirstlane(a.order[blockIdx.x])
+                             : ((int)(blockIdx.x % (unsigned)P) * a.q_chunks + rest / n_splits) * n_splits +
+                                   (n_splits - 1 - rest % n_splits);
+    split = code % n_splits;
+    qc = code / n_splits % a.q_chunks;
+    const int pair_id = code / n_splits / a.q_chunks;
+    g = pair_id % a.Hkv;
+    b = pair_id / a.Hkv;
+    gam = a.gamma[b];
+    L = a.kv_len[b];
+    pair = (size_t)pair_id;
+  }
+  const int job = (b * a.Hkv + g) * a.q_chunks + qc;
   const int G = a.Hq / a.Hkv;
   const int R = G * (a.gmax + 1);
-  const int gam = a.gamma[b];
-  const int L = a.kv_len[b];
   const bool valid = gam >= 0 && gam <= a.gmax && L >= gam + 1 && L <= a.L_cap;
   if (!valid && split == 0 && qc == 0 && g == 0 && threadIdx.x == 0 && a.status) {
     atomicOr(a.status, (gam < 0 || gam > a.gmax) ? SR_ST_GAMMA : SR_ST_KVLEN);
@@ -131,11 +220,8 @@ attn_kv4_kernel(Kv4Args a) {
   const int row0 = qc * MQ;
   const int row_end = min(R, row0 + MQ);
   const int Mb = valid ? G * (gam + 1) : 0;
-  const int window = a.window > 0 ? a.window : 0x7fffffff;
-  const int sinks = a.sinks;
   const int causal0 = valid ? L - gam - 1 : 0;  // cache position of new row 0
   const Reach<kTile> reach(causal0, valid ? L : 0, window, sinks);
-  const int tiles_per = a.split_keys / kTile;
   const int ns = (reach.tiles + tiles_per - 1) / tiles_per;  // splits that hold keys
   const bool work = row0 < Mb && split < ns;
 
@@ -406,7 +492,7 @@ attn_kv4_kernel(Kv4Args a) {
   for (int qg = 0; qg < NQ; ++qg) l_run[qg] = sum_across_rows(l_run[qg]);
   __syncthreads();
 
-  const JobRows J{row0, row_end, Mb, R, split, ns, a.n_splits, job, P, (size_t)(b * a.Hkv + g)};
+  const JobRows J{row0, row_end, Mb, R, split, ns, n_splits, job, pairs, pair};
   merge_and_store<typename LL::Merge, D, NQ, 1, LL::kBytes, true>(lds, o, m_run, l_run, J, a.part_o, a.part_ml, a.counters, store);
 }
 
@@ -471,17 +557,30 @@ int attention_kv4_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_r
   // and 287), and one with two row blocks and more than four workgroups per CU, for a
   // third wave per SIMD (256 sequences of 2048 keys, gamma 5: 121 and 135; 24 ragged ones,
   // 2.25 workgroups per CU: 46 and 39).
-  const long n_jobs = (long)plan->n_splits * pairs;
+  // Up to 64 sequences on no more workgroups than CUs: the kernel deals them by the
+  // lengths, which the host does not know, to two workgroups per CU (32/8 heads of 128,
+  // gamma 5, us with the splits above and dealt: 18 sequences of 4456 keys 39 and 28, 12 of
+  // 256 to 8192 30 and 27, 24 of 256 to 8192 39 and 37, one of 512 10.8 and 11.3). With more, a
+  // ragged batch has few splits to give away: 46 sequences of 1292 to 15505 89 and 111.
+  plan->units = 0;
+  if (B <= kMaxDealt && pairs <= cus && L > 4 * kMergeKeys) {
+    const int tiles = (L + kTile - 1) / kTile, least = least_tiles(tiles);
+    const long room = 2L * cus / (Hkv * plan->q_chunks), need = (long)B * ((tiles + least - 1) / least);
+    plan->units = (int)(need < room ? need : room);
+    plan->n_splits = (plan->units + B - 1) / B;
+  }
+  const long n_jobs = plan->units > 0 ? (long)plan->units * Hkv * plan->q_chunks : (long)plan->n_splits * pairs;
   plan->ring = plan->nq == 3 || (plan->nq == 2 && n_jobs > 4L * cus) ? 1 : 2;
   const long target =
       (long)cus * resident_per_cu((const void*)pick_kv4(D, plan->nq, plan->ring, plan->q_chunks), 64 * kWaves, 0);
   // [arrival counters, one per 128-byte line][partial o][partial (m, l)][order]
   const size_t counters = (size_t)pairs * kCounterStride * sizeof(uint32_t);
   plan->part_offset = counters;
-  size_t bytes = plan->n_splits > 1 ? counters + (size_t)B * Hkv * plan->n_splits * R * (D + 2) * sizeof(float) : 0;
+  const size_t records = plan->units > 0 ? (size_t)Hkv * plan->units : (size_t)B * Hkv * plan->n_splits;
+  size_t bytes = plan->units > 0 || plan->n_splits > 1 ? counters + records * R * (D + 2) * sizeof(float) : 0;
   // (Up to 1024 keys what it balances is less than the order kernel's 5 us: 256
   // sequences of 100 to 300 keys 36.6 us with it, 34.1 without, of 100 to 700 45.3 and 43.6.)
-  plan->ordered = n_jobs > target && L > 1024 ? 1 : 0;
+  plan->ordered = n_jobs > target && L > 1024 && plan->units == 0 ? 1 : 0;
   plan->order_offset = (bytes + 15) / 16 * 16;
   if (plan->ordered) bytes = plan->order_offset + (size_t)n_jobs * sizeof(int32_t);
   plan->workspace_bytes = bytes;
@@ -495,7 +594,8 @@ int launch_attention_kv4(const void* q, const void* k_codes, const void* k_power
                          hipStream_t stream) {
   const int R = Hq / Hkv * (gamma_max + 1);
   float* part_o = workspace ? (float*)((char*)workspace + plan.part_offset) : nullptr;
-  float* part_ml = part_o ? part_o + (size_t)B * Hkv * plan.n_splits * R * D : nullptr;
+  const size_t records = plan.units > 0 ? (size_t)Hkv * plan.units : (size_t)B * Hkv * plan.n_splits;
+  float* part_ml = part_o ? part_o + records * R * D : nullptr;
   int32_t* order = plan.ordered ? (int32_t*)((char*)workspace + plan.order_offset) : nullptr;
   if (order && launch_attention_order(kv_len, gamma, B, gamma_max, Hkv, plan.q_chunks, L_cap, window, sinks, kTile,
                                       plan.split_keys, plan.n_splits, order, stream) != SR_OK)
@@ -503,8 +603,8 @@ int launch_attention_kv4(const void* q, const void* k_codes, const void* k_power
   const Kv4Args a{(const uint16_t*)q, (const uint8_t*)k_codes, (const uint8_t*)k_powers, (const uint8_t*)v_codes,
                   (const uint8_t*)v_powers, cache_mask, kv_len, gamma, out, out_bf16, part_o, part_ml,
                   (uint32_t*)workspace, order, B, gamma_max, Hq, Hkv, L_cap, window, sinks, scale * kLog2e,
-                  plan.split_keys, plan.n_splits, plan.q_chunks, status};
-  const dim3 grid((unsigned)((long)plan.n_splits * plan.q_chunks * B * Hkv));
+                  plan.split_keys, plan.n_splits, plan.q_chunks, plan.units, status};
+  const dim3 grid((unsigned)((plan.units > 0 ? (long)plan.units : (long)plan.n_splits * B) * plan.q_chunks * Hkv));
   hipLaunchKernelGGL(pick_kv4(D, plan.nq, plan.ring, plan.q_chunks), grid, dim3(64 * kWaves), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SR_OK : SR_ELAUNCH;
 }

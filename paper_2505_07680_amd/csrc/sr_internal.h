@@ -266,6 +266,7 @@ struct AttentionPlan {
   int n_splits;    // splits along the cache
   int follow;      // the softmax references follow the tiles
   int ring;        // tiles in flight per wave (4-bit cache)
+  int units;       // > 0: (sequence, split) pairs that the launch has room for, dealt by the lengths (4-bit cache)
   size_t part_offset;  // byte offset of the split partials in the workspace
   int ordered;         // more workgroups than fit at once: dispatched longest job first
   size_t order_offset;  // byte offset of the dispatch order in the workspace

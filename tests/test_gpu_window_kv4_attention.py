@@ -348,3 +348,31 @@ def test_forms_of_many_rows(B, Hq, Hkv, D, G1, cap, win):
     x = Inputs(rng, B, G1, Hq, Hkv, D, cap, ctx, gamma=gamma, holes=0.05, four=False)
     say(f"B={B} rows={Hq // Hkv * G1} D={D} window={win}")
     x.compare("window", win, 5)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,G1,cap,win", [(2, 4, 4, 64, 2, 3000, 0), (17, 8, 2, 64, 3, 1500, 0), (64, 4, 4, 64, 1, 700, 0),
+                                                   (65, 4, 2, 64, 1, 700, 0), (63, 3, 3, 128, 2, 600, 0), (30, 12, 3, 64, 17, 500, 0),
+                                                   (9, 8, 1, 128, 5, 5000, 0), (20, 6, 3, 64, 4, 2500, 900), (1, 4, 2, 64, 3, 20000, 0)])
+def test_kv4_batches_dealt_by_their_lengths(B, Hq, Hkv, D, G1, cap, win):
+    """One long sequence among short ones, all alike, and bad ones in between, over one workspace."""
+    rng = np.random.default_rng(17)
+    x = Inputs(rng, B, G1, Hq, Hkv, D, cap, [cap - G1] * B, holes=0.03)
+    x.upload("kv4")
+    ws = x.workspace("kv4", win, 4)
+    for lengths in ("alike", "one long", "ragged", "bad"):
+        x.gamma[:] = rng.integers(0, G1, B)
+        low = rng.integers(0, 40, B)
+        ctx = {"alike": np.full(B, cap - G1), "one long": low, "ragged": rng.integers(0, cap - G1 + 1, B), "bad": low}[lengths]
+        ctx[B // 2] = cap - G1
+        x.kv_len[:] = ctx + x.gamma + 1
+        if lengths == "bad":
+            x.gamma[::3] = G1
+            x.kv_len[1::5] = cap + 1
+        x.dlen, x.dgam = dev(x.kv_len), dev(x.gamma)
+        out = torch.full((B, G1, Hq, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        say(f"B={B} {Hq}/{Hkv}x{D} cap={cap} {lengths}")
+        x.call("kv4", win, 4, out, ws, st)
+        ref, size, rst = x.reference("kv4", win, 4)
+        assert int(st) == rst
+        check(out, ref, size)
