@@ -28,7 +28,7 @@
 //
 // With one query row per head HBM bounds it (256 sequences of 4096 keys, 32/8
 // heads of 128: 179 to 198 us, 5.8 to 6.4 TB/s); with more rows the instructions of
-// two waves per SIMD do: 256 of 256 to 8192 keys, gamma 1 to 8, 246 us, 4.9 TB/s,
+// two waves per SIMD do: 256 of 256 to 8192 keys, gamma 1 to 8, 242 us, 5.0 TB/s,
 // vector units 47% busy, matrix units 24%, LDS 30% (over a bf16 cache 730 us). 16
 // sequences of 2048, gamma 5, take 19 us, half of it latency: start, lengths and
 // first loads before the loop, the merge of four splits after it.
