@@ -118,18 +118,20 @@ int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_rows,
   // of 1024 positions, 64 rows, 20.0 and 13.6; 16 of 1024 28.8 and 23.4, of 3000
   // 45.5 and 53.7; 32 of 512 25.2 and 24.3, of 640 26.6 and 29.9; 40 of 2048,
   // 72 rows, 118 and 98, 136 rows 164 and 120; 256 of 512, 72 rows, 217 and 176.)
+  bool chunked = false;
   if (window > 0 && plan->qg > 1) {
     const int chunks = (R + 16 * kMaxNQ - 1) / (16 * kMaxNQ);
     const long jobs = (long)B * Hkv * plan->q_chunks;
     const bool even = jobs <= cus && cus % jobs == 0;
     if (!even || chunks < kMaxQG * plan->q_chunks || jobs * L_cap <= 600l * cus) {
+      chunked = true;
       plan->qg = 1;
       plan->q_chunks = chunks;
       plan->nq = ((R + chunks - 1) / chunks + 15) / 16;
     }
   }
   const int threads = plan->qg == 1 ? Shape<1>::kThreads : Shape<kMaxQG>::kThreads;
-  const int per_cu = resident_per_cu((const void*)(window > 0 ? window_kernel(D, plan->nq, plan->qg, plan->q_chunks)
+  const int per_cu = resident_per_cu((const void*)(window > 0 ? window_kernel(D, plan->nq, plan->qg, plan->q_chunks, false)
                                                                  : pick_split(D, plan->nq, plan->qg, plan->q_chunks, false)), threads, 0);
   const long pairs = (long)B * Hkv * plan->q_chunks;
   const long target = (long)cus * per_cu;
@@ -199,8 +201,18 @@ int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_rows,
   // wave with a lazy reference. Fewer and longer splits would have fewer of
   // them (64 to 8192 normal keys: 1.05e-3 off the 64-bit result with one tile
   // per wave, 1.5e-3 with three), so there the reference follows the tiles
-  // (one such key per tile whatever the length: 1.05e-3 again).
+  // (one such key per tile whatever the length: 1.05e-3 again). With a window that costs
+  // a call 3 to 10% (one sequence of 8192 positions, 72 rows, 25.4 and 26.6 us).
   plan->follow = few ? 1 : 0;
+  // Rows in chunks with a window are as exact as the two groups without one: where those
+  // follow, or leave a wave one tile, a wave of several tiles follows here. (2 sequences
+  // of 2048 keys, 72 rows: 1.52e-3 off where the reference is lazy, 1.01e-3 where it follows.)
+  if (chunked) {
+    AttentionPlan groups;
+    const int rc = plan->split_keys > kTileKeys ? attention_plan(B, gamma_max, Hq, Hkv, D, L_cap, 0, 0, &groups) : SR_OK;
+    if (rc != SR_OK) return rc;
+    plan->follow = plan->split_keys > kTileKeys && (groups.follow || groups.split_keys <= kTileKeys) ? 1 : 0;
+  }
   // [arrival counters: B*Hkv*q_chunks, one per 128-byte line][partial o][partial (m, l)][order]
   const size_t counters = (size_t)B * Hkv * plan->q_chunks * kCounterStride * sizeof(uint32_t);
   plan->part_offset = counters;
@@ -243,7 +255,7 @@ int launch_verify_attention(const void* q, const void* k_cache, const void* v_ca
   if (order && launch_attention_order(kv_len, gamma, B, gamma_max, Hkv, plan.q_chunks, L_cap, window, sinks, kWaveKeys,
                                       plan.split_keys, plan.n_splits, order, stream) != SR_OK)
     return SR_ELAUNCH;
-  const SplitKernel kernel = window > 0 ? window_kernel(D, plan.nq, plan.qg, plan.q_chunks)
+  const SplitKernel kernel = window > 0 ? window_kernel(D, plan.nq, plan.qg, plan.q_chunks, plan.follow != 0)
                                         : pick_split(D, plan.nq, plan.qg, plan.q_chunks, plan.follow != 0);
   hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, (const uint16_t*)q, (const uint16_t*)k_cache,
                      (const uint16_t*)v_cache, cache_mask, kv_len, gamma, out, out_bf16, part_o, part_ml, counters,

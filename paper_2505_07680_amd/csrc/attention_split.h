@@ -48,8 +48,9 @@
 // the cache's first `sinks`. Only the tiles that hold such keys are taken: they
 // are numbered without the gap between the sinks and row 0's first key, and
 // splits and streams deal those numbers as they deal all tiles otherwise. V rows
-// that no row sees are zeroed like masked ones. Its softmax takes a row's maximum
-// and sum across lanes only when the reference grows and at the end, masks by
+// that no row sees are zeroed like masked ones. Its softmax takes a row's sum across
+// lanes at the end and its maximum only when the reference grows (or follows the
+// tiles, where the call without a window would have it follow), masks by
 // putting -infinity in the scores' place, and with one query group leaves row
 // blocks without live rows out of the products too (the loop is compiled for
 // each number of them): 64 sequences of 1024 positions, gamma 1 to 8, 58 -> 53 us,
@@ -266,10 +267,10 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
     st.mbyte = mload[min(kb0 + (lane & (kWaveKeys - 1)), L - 1)];
   };
   // With a window: P of the scores score(qg, e), e < N, of a row's N keys per lane,
-  // two at a time to put(qg, pair, bf16x2). A row's reference stands until a score
+  // two at a time to put(qg, pair, bf16x2). Lazy, a row's reference stands until a score
   // exceeds it by more than 2^kLazy; only then do its four lanes need their common
   // maximum. Each lane sums its own keys; the row's lanes are added up at the end.
-  auto lazy_softmax = [&](auto blocks, auto score, auto count, auto put) __attribute__((always_inline)) {
+  auto window_softmax = [&](auto blocks, auto score, auto count, auto put) __attribute__((always_inline)) {
     constexpr int NL = decltype(blocks)::value;
     constexpr int N = decltype(count)::value;
     float mt[NL];
@@ -282,11 +283,11 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
       mt[qg] *= scale_log2;
       over |= mt[qg] > m_run[qg] + kLazy;
     }
-    if (rare(__ballot(over) != 0ull)) {
+    if (FOLLOW || rare(__ballot(over) != 0ull)) {
 #pragma unroll
       for (int qg = 0; qg < NL; ++qg) {
         const float m = max_across_rows(mt[qg]);
-        const float mref = m > m_run[qg] + kLazy ? m : m_run[qg];
+        const float mref = next_ref<FOLLOW>(m, m_run[qg], m > m_run[qg] + (FOLLOW ? kLazyFollow : kLazy));
         const float alpha = m_run[qg] == mref ? 1.f : exp2_hw(m_run[qg] - mref);
         m_run[qg] = mref;
         l_run[qg] *= alpha;
@@ -374,8 +375,8 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
           }
         }
       }
-      lazy_softmax(blocks, [&](int qg, int e) __attribute__((always_inline)) { return sacc[qg][e]; },
-                   std::integral_constant<int, 4>{},
+      window_softmax(blocks, [&](int qg, int e) __attribute__((always_inline)) { return sacc[qg][e]; },
+                     std::integral_constant<int, 4>{},
                    [&](int qg, int pair, uint32_t two) __attribute__((always_inline)) {
                      u32x2 w = __builtin_bit_cast(u32x2, pb[qg]);
                      w[pair] = two;
@@ -533,7 +534,7 @@ attn_split_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
             }
           }
         }
-        lazy_softmax(blocks, [&](int qg, int e) __attribute__((always_inline)) { return sacc[e / 4][qg][e % 4]; },
+        window_softmax(blocks, [&](int qg, int e) __attribute__((always_inline)) { return sacc[e / 4][qg][e % 4]; },
                      std::integral_constant<int, 8>{},
                      [&](int qg, int pair, uint32_t two) __attribute__((always_inline)) {
                        u32x4 w = __builtin_bit_cast(u32x4, pb[qg]);

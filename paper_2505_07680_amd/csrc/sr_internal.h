@@ -277,7 +277,7 @@ struct AttentionPlan {
 typedef void (*SplitKernel)(const uint16_t*, const uint16_t*, const uint16_t*, const uint8_t*,
                             const int32_t*, const int32_t*, void*, bool, float*, float*, uint32_t*,
                             const int32_t*, int, int, int, int, int, int, int, float, int, int, int, int32_t*);
-SplitKernel window_kernel(int D, int nq, int qg, int q_chunks);
+SplitKernel window_kernel(int D, int nq, int qg, int q_chunks, bool follow);
 
 // window 0: all keys, else the last `window` positions of each row and the first `sinks`
 int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int L_cap, int window, int sinks, AttentionPlan* plan);
