@@ -407,7 +407,8 @@ int specrouter_kv_compact(void* k_cache, void* v_cache, uint8_t* cache_mask, int
  *              be q / k themselves where those are contiguous, else they must
  *              not overlap them
  * Rows i > gamma_b, and all rows of a sequence with bad data, are neither read
- * nor written. Computed in fp32 and rounded to bf16 once.
+ * nor written. Computed in fp32 and rounded to bf16 once; a head of any finite
+ * magnitude has its norm (squares outside fp32's range are scaled first).
  */
 int specrouter_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* q_weight,
                             const void* k_weight, int weight_dtype, float eps, const float* rope_table,

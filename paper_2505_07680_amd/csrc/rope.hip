@@ -31,6 +31,9 @@ constexpr int kRopeThreads = 256;
 // and 4.2, 1443 tokens 9.7 and 11.1, 4096 tokens 20.7 and 21.5);
 // streamed from HBM it is the other way round (333 MB 64 and 58, 1.2 GB 195 and 190).
 constexpr int head_steps(int caching) { return caching == kPass ? 4 : 2; }
+// A mean of squares from here to 32 bits' largest has all its bits: a square that counts, from
+// 2^-24 of the largest on, is not below 2^-126.
+constexpr float kLeastMean = 0x1p-96f;
 
 __device__ __forceinline__ float lane_f32(float x, int src_lane) {
   return __int_as_float(__builtin_amdgcn_ds_bpermute(src_lane * 4, __float_as_int(x)));
@@ -131,7 +134,35 @@ qk_norm_rope_kernel(const uint16_t* q, int64_t q_stride, const uint16_t* k, int6
     ss += perm_f32<dpp::kXor2>(ss);
     ss += perm_f32<dpp::kHalfMirror>(ss);
     if constexpr (kLanes == 16) ss += perm_f32<dpp::kMirror>(ss);
-    const float rs = rsqrtf(ss * (1.f / D) + eps);
+    float ms = ss * (1.f / D) + eps;
+    // Squares beyond 32 bits' range, or so small that they lose bits: the head again, divided
+    // by the power of two above its largest magnitude (and above sqrt(eps)), which is exact.
+    const bool scaled = __float_as_uint(ms) - __float_as_uint(kLeastMean) >= 0x7f800000u - __float_as_uint(kLeastMean);
+    if (__builtin_expect(__ballot(scaled) != 0ull, 0)) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
+      top = max(top, perm_u32<dpp::kXor1>(top));
+      top = max(top, perm_u32<dpp::kXor2>(top));
+      top = max(top, perm_u32<dpp::kHalfMirror>(top));
+      if constexpr (kLanes == 16) top = max(top, perm_u32<dpp::kMirror>(top));
+      // (an infinity or a NaN, and a head without a norm, stay as they are)
+      const bool at_all = scaled && top < 0x7f800000u && (is_q ? qw != nullptr : kw != nullptr);
+      const int of_eps = eps > 0.f ? (__builtin_amdgcn_frexp_expf(eps) + 1) / 2 : -1000;
+      const int power = at_all ? max(__builtin_amdgcn_frexp_expf(__uint_as_float(top)), of_eps) : 0;
+      ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        y[e] = ldexpf(y[e], -power);
+        ss = fmaf(y[e], y[e], ss);
+      }
+      ss += perm_f32<dpp::kXor1>(ss);
+      ss += perm_f32<dpp::kXor2>(ss);
+      ss += perm_f32<dpp::kHalfMirror>(ss);
+      if constexpr (kLanes == 16) ss += perm_f32<dpp::kMirror>(ss);
+      ms = ss * (1.f / D) + ldexpf(eps, -2 * power);
+    }
+    const float rs = rsqrtf(ms);
     if (is_q ? qw != nullptr : kw != nullptr) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] *= rs * (is_q ? wq[e] : wk[e]);
