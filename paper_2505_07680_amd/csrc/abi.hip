@@ -332,7 +332,7 @@ int specrouter_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(rope_table) ||
       !aligned16(q_weight) || !aligned16(k_weight))
     return SR_EINVAL;
-  // in place only where input and output rows are the same rows
+  // in place only where input and output rows are the same rows (of q and k at one address one may be)
   if (q_out == k_out || (q != k && (q_out == k || k_out == q))) return SR_EINVAL;
   if ((q_out == q && q_stride != (int64_t)Hq * D) || (k_out == k && k_stride != (int64_t)Hkv * D)) return SR_EINVAL;
   return sr::launch_qk_norm_rope(q, q_stride, k, k_stride, q_weight, k_weight, weight_dtype == SR_F32, eps, rope_table,

@@ -202,6 +202,19 @@ int launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t 
                         const void* k_weight, bool w_f32, float eps, const float* table, int max_positions, int rot,
                         bool adjacent, const int32_t* position, const int32_t* gamma, void* q_out, void* k_out, int B,
                         int gamma_max, int Hq, int Hkv, int D, int32_t* status, hipStream_t stream) {
+  // Queries and keys from the same rows, one of them in place: the other first, in a launch of its own.
+  if (q == k && (q_out == q || k_out == k)) {
+    const auto queries = [&] {
+      return launch_qk_norm_rope(q, q_stride, nullptr, 0, q_weight, nullptr, w_f32, eps, table, max_positions, rot,
+                                 adjacent, position, gamma, q_out, k_out, B, gamma_max, Hq, 0, D, status, stream);
+    };
+    const auto keys = [&] {
+      return launch_qk_norm_rope(nullptr, 0, k, k_stride, nullptr, k_weight, w_f32, eps, table, max_positions, rot,
+                                 adjacent, position, gamma, q_out, k_out, B, gamma_max, 0, Hkv, D, status, stream);
+    };
+    const int rc = q_out == q ? keys() : queries();
+    return rc != SR_OK ? rc : q_out == q ? queries() : keys();
+  }
   const Caching caching = caching_of((long)B * (gamma_max + 1) * (Hq + Hkv) * D * 4);
   const int per_wave = 64 / (D / 8) * head_steps(caching);
   const int parts = (Hq + Hkv + per_wave - 1) / per_wave;
