@@ -491,6 +491,19 @@ def _row_stride(t, rows, H, D, name):
     return s1 if rows > 1 else s0 if B > 1 else H * D
 
 
+def _meets(out, size, x, stride, width, rows):
+    """Whether the bytes [out, out + size) touch one of `rows` runs of `width` bytes that lie `stride` apart from x on."""
+    i = max(0, (out - x - width) // max(stride, 1) + 1)  # the first run that ends behind out
+    return i < rows and x + i * stride < out + size
+
+
+def _apart(name, out, size, **others):
+    """Raise where an output of `size` bytes meets another argument, name=(address, stride, width, rows)."""
+    for other, rows in others.items():
+        if _meets(out, size, *rows):
+            raise ValueError(f"{name} must not overlap {other}")
+
+
 def specrouter_qk_norm_rope(q, k, q_weight, k_weight, eps, rope_table, position, gamma, q_out, k_out,
                             interleaved=False, status=None):
     """q [B, rows, Hq, D] and k [B, rows, Hkv, D] bf16 (views of one projection
@@ -520,10 +533,21 @@ def specrouter_qk_norm_rope(q, k, q_weight, k_weight, eps, rope_table, position,
                 rope_table=(rope_table, None, (torch.float32,), True),
                 q_weight=(q_weight, (D,), _OUT, True),
                 k_weight=(k_weight, (D,), _OUT if q_weight is None else (w.dtype,), True), status=(status, None, (_INT32,), True))
+    x, y, xo, yo = q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr()
+    xs = Hq * D if q.is_contiguous() else _row_stride(q, rows, Hq, D, "q")
+    ys = Hkv * D if k.is_contiguous() else _row_stride(k, rows, Hkv, D, "k")
+    n = 2 * B * rows
+    xe, ye, xoe, yoe = x + n * xs, y + n * ys, xo + n * Hq * D, yo + n * Hkv * D  # (past the last row of each)
+    if (xo < xe and x < xoe and xo != x or xo < ye and y < xoe or yo < xe and x < yoe
+            or yo < ye and y < yoe and yo != y or xo < yoe and yo < xoe):
+        # (in place, where the library checks the strides: each its own rows, or those of both)
+        ins = dict(q=(x, 2 * xs, 2 * Hq * D, B * rows), k=(y, 2 * ys, 2 * Hkv * D, B * rows))
+        _apart("q_out", xo, xoe - xo, k_out=(yo, 1, yoe - yo, 1),
+               **{i: v for i, v in ins.items() if xo != x or i == "k" and x != y})
+        _apart("k_out", yo, yoe - yo, **{i: v for i, v in ins.items() if yo != y or i == "q" and x != y})
     rc = (_lib or load()).specrouter_qk_norm_rope(
-        q.data_ptr(), _row_stride(q, rows, Hq, D, "q"), k.data_ptr(), _row_stride(k, rows, Hkv, D, "k"), _ptr(q_weight), _ptr(k_weight), code,
-        eps, rope_table.data_ptr(), max_positions, rot, 1 if interleaved else 0, position.data_ptr(), gamma.data_ptr(),
-        q_out.data_ptr(), k_out.data_ptr(), B, rows - 1, Hq, Hkv, D, _ptr(status),
+        x, xs, y, ys, _ptr(q_weight), _ptr(k_weight), code, eps, rope_table.data_ptr(), max_positions, rot,
+        1 if interleaved else 0, position.data_ptr(), gamma.data_ptr(), xo, yo, B, rows - 1, Hq, Hkv, D, _ptr(status),
         torch._C._cuda_getCurrentRawStream(here))
     if rc:
         _check(rc, "specrouter_qk_norm_rope")
@@ -564,10 +588,27 @@ def specrouter_kv4_append(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_pow
                 kv_len=(kv_len, (B,), (_INT32,), True), shared_len=(shared_len, (1,), (_INT32,), True),
                 k_seen=(k_seen, ns, (_BF16,), True), v_seen=(v_seen, ns, (_BF16,), True),
                 status=(status, None, (_INT32,), True))
+    x, xs, y, ys = (k_new.data_ptr(), _row_stride(k_new, rows, Hkv, D, "k_new"), v_new.data_ptr(),
+                    _row_stride(v_new, rows, Hkv, D, "v_new"))
+    kc, kp, vc, vp = k_codes.data_ptr(), k_powers.data_ptr(), v_codes.data_ptr(), v_powers.data_ptr()
+    ks, vs = _ptr(k_seen), _ptr(v_seen)
+    if ks or vs:
+        n, codes = 2 * B * rows, B * Hkv * L_cap * D // 2
+        powers, size = codes // 16, n * Hkv * D
+        xe, ye, kce, kpe, vce, vpe = x + n * xs, y + n * ys, kc + codes, kp + powers, vc + codes, vp + powers
+        for name, o in (("k_seen", ks), ("v_seen", vs)):
+            oe = (o or 0) + size
+            if o and (o < xe and x < oe and o != x or o < ye and y < oe and o != y or o < kce and kc < oe
+                      or o < kpe and kp < oe or o < vce and vc < oe or o < vpe and vp < oe
+                      or vs and o < vs + size and vs < oe and o != vs):
+                others = dict(k_new=(x, 2 * xs, 2 * Hkv * D, B * rows), v_new=(y, 2 * ys, 2 * Hkv * D, B * rows),
+                              k_codes=(kc, 1, codes, 1), k_powers=(kp, 1, powers, 1), v_codes=(vc, 1, codes, 1),
+                              v_powers=(vp, 1, powers, 1), v_seen=(vs or 0, 1, size if vs else 0, 1))
+                # (at the start of one of these: the library's to refuse, or in place)
+                _apart(name, o, size, **{i: v for i, v in others.items() if v[0] != o})
     rc = (_lib or load()).specrouter_kv4_append(
-        k_new.data_ptr(), _row_stride(k_new, rows, Hkv, D, "k_new"), v_new.data_ptr(), _row_stride(v_new, rows, Hkv, D, "v_new"), gamma.data_ptr(),
-        k_codes.data_ptr(), k_powers.data_ptr(), v_codes.data_ptr(), v_powers.data_ptr(), _ptr(cache_mask),
-        kv_len.data_ptr(), _ptr(shared_len), _ptr(k_seen), _ptr(v_seen), B, rows - 1, Hkv, D, L_cap, _ptr(status),
+        x, xs, y, ys, gamma.data_ptr(), kc, kp, vc, vp, _ptr(cache_mask),
+        kv_len.data_ptr(), _ptr(shared_len), ks, vs, B, rows - 1, Hkv, D, L_cap, _ptr(status),
         torch._C._cuda_getCurrentRawStream(here))
     if rc:
         _check(rc, "specrouter_kv4_append")
