@@ -59,8 +59,8 @@ def parse():
 # Sources whose kernels each entry point launches: HBM byte counters taken
 # for an older version of them no longer describe the code that runs.
 KERNEL_SOURCES = {
-    "verify_attention": ["attention.hip", "sr_internal.h"],
-    "accept_and_diverge": ["accept.hip", "sr_internal.h"],
+    "verify_attention": ["attention.hip", "attention_split.h", "attention_common.h", "sr_internal.h"],
+    "accept_and_diverge": ["accept.hip", "filter.inc", "sr_internal.h"],
     "rollback": ["rollback.hip", "sr_internal.h"],
     "accept_filter": ["accept.hip", "filter.inc", "sr_internal.h"],
 }
