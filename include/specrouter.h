@@ -138,12 +138,15 @@ int specrouter_verify_attention(const void* q, const void* k_cache, const void* 
 /* Verification attention with a sliding window and sinks: as
  * specrouter_verify_attention, but the row at cache position pos sees, of the
  * keys j <= pos with cache_mask[b][j] != 0, those with j > pos - window or
- * j < sinks. Positions are cache rows, masked ones counted. Only the rows that
- * some new row can see are read: at most window + gamma_b + sinks per sequence
- * and kv head, and what lies between the sinks and the window is ignored
- * whatever it holds. NaN in a key that a row sees gives NaN in that row; NaN or
- * infinity in V of such a key gives NaN or infinity in its column there, and may
- * give NaN in the sequence's other rows too, as 0 times it is NaN.
+ * j < sinks. Positions are cache rows, masked ones counted. Of the cache rows
+ * below kv_len_b, the aligned tiles of 16 (of 32 over a 4-bit cache) that hold a
+ * key which some new row can see are read: at most window + gamma_b + sinks rows
+ * and 30 (62) more per sequence and kv head, once for every 48 or 96 query rows
+ * of the head. Rows of them that no new row sees are ignored whatever they hold,
+ * as is what is not read between the sinks and the window. NaN in a key that a
+ * row sees gives NaN in that row; NaN or infinity in V of such a key gives NaN or
+ * infinity in its column there, and may give NaN in the sequence's other rows
+ * too, as 0 times it is NaN.
  *
  * window     >= 1 (from L_cap on it hides nothing); sinks >= 0; else SR_EINVAL
  * out        [B][gamma_max+1][Hq][D] of out_dtype: SR_F32, or SR_BF16 (the same
