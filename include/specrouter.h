@@ -449,7 +449,9 @@ int specrouter_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
  *               contiguous, else they must not overlap any other argument
  * shared_len    i32 [1] or NULL, not an element of kv_len
  * Everything else as for specrouter_kv_append; lengths, mask and rollback of
- * such a cache are those of a bf16 one.
+ * such a cache are those of a bf16 one. specrouter_kv_compact takes bf16 only:
+ * the masked holes that a shared cursor leaves in a 4-bit cache stay, and count
+ * towards L_cap, until the sequence starts again.
  */
 int specrouter_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
                           const int32_t* gamma, void* k_codes, void* k_powers, void* v_codes, void* v_powers,
