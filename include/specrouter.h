@@ -464,7 +464,10 @@ int specrouter_kv4_append(const void* k_new, int64_t k_stride, const void* v_new
  * no new row sees are ignored whatever they hold (NaN in V that one row sees: as
  * for the window call). out_dtype as for the window
  * call; workspace of specrouter_verify_attention_kv4_workspace_size() bytes for
- * the same arguments, zero-filled before its first use. Repeated calls give
+ * the same arguments, zero-filled before its first use. Precision: bf16 products,
+ * fp32 accumulation and softmax, the weights rounded to bf16 (over normal keys
+ * 1.5e-3 of the values in all; specrouter_verify_attention comes to 1.0e-3 for
+ * small batches, whose weights it rounds more carefully). Repeated calls give
  * identical bits; where a sequence's keys are split, and so its last bits, may
  * depend on the lengths of the others in its batch.
  */

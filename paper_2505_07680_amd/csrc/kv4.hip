@@ -15,10 +15,10 @@
 // stores are one run of the head's slab.
 //
 // Prompts are bound by HBM and their many short runs (8 KB to 2 KB apart in what is
-// read, 16 bytes a row's powers): 8 of 2048 to 4095 rows, 8 heads of 128, with
-// the values that attention will see, 228 MB, 40 us in the rows' kernel (5.7 TB/s)
-// and 4 in the lengths'. A step's rows are bound by latency: 5.2 us for 256
-// sequences (13 MB), of which the launch is about half.
+// read; powers of 4 bytes a row at D = 128, 2 at 64, 16 to a wave's rows): 8 of 2048 to
+// 4095 rows, 8 heads of 128, with the values that attention will see, 228 MB, 40 us in
+// the rows' kernel (5.7 TB/s) and 4 in the lengths'. A step's rows are bound by latency:
+// 5.2 us for 256 sequences (13 MB), of which the launch is about half.
 
 #include "caching.h"
 
