@@ -588,27 +588,29 @@ def specrouter_kv4_append(k_new, v_new, gamma, k_codes, k_powers, v_codes, v_pow
                 kv_len=(kv_len, (B,), (_INT32,), True), shared_len=(shared_len, (1,), (_INT32,), True),
                 k_seen=(k_seen, ns, (_BF16,), True), v_seen=(v_seen, ns, (_BF16,), True),
                 status=(status, None, (_INT32,), True))
-    x, xs, y, ys = (k_new.data_ptr(), _row_stride(k_new, rows, Hkv, D, "k_new"), v_new.data_ptr(),
-                    _row_stride(v_new, rows, Hkv, D, "v_new"))
+    x, y = k_new.data_ptr(), v_new.data_ptr()
+    xs = Hkv * D if k_new.is_contiguous() else _row_stride(k_new, rows, Hkv, D, "k_new")
+    ys = Hkv * D if v_new.is_contiguous() else _row_stride(v_new, rows, Hkv, D, "v_new")
     kc, kp, vc, vp = k_codes.data_ptr(), k_powers.data_ptr(), v_codes.data_ptr(), v_powers.data_ptr()
-    ks, vs = _ptr(k_seen), _ptr(v_seen)
+    ks = 0 if k_seen is None else k_seen.data_ptr()
+    vs = 0 if v_seen is None else v_seen.data_ptr()
     if ks or vs:
         n, codes = 2 * B * rows, B * Hkv * L_cap * D // 2
         powers, size = codes // 16, n * Hkv * D
         xe, ye, kce, kpe, vce, vpe = x + n * xs, y + n * ys, kc + codes, kp + powers, vc + codes, vp + powers
-        for name, o in (("k_seen", ks), ("v_seen", vs)):
-            oe = (o or 0) + size
-            if o and (o < xe and x < oe and o != x or o < ye and y < oe and o != y or o < kce and kc < oe
-                      or o < kpe and kp < oe or o < vce and vc < oe or o < vpe and vp < oe
-                      or vs and o < vs + size and vs < oe and o != vs):
+        for o in (ks, vs):
+            oe = o + size
+            if (x < oe and o < xe and o != x or y < oe and o < ye and o != y or kc < oe and o < kce
+                    or kp < oe and o < kpe or vc < oe and o < vce or vp < oe and o < vpe
+                    or vs < oe and o < vs + size and o != vs):
                 others = dict(k_new=(x, 2 * xs, 2 * Hkv * D, B * rows), v_new=(y, 2 * ys, 2 * Hkv * D, B * rows),
                               k_codes=(kc, 1, codes, 1), k_powers=(kp, 1, powers, 1), v_codes=(vc, 1, codes, 1),
-                              v_powers=(vp, 1, powers, 1), v_seen=(vs or 0, 1, size if vs else 0, 1))
+                              v_powers=(vp, 1, powers, 1), v_seen=(vs, 1, size, 1))
                 # (at the start of one of these: the library's to refuse, or in place)
-                _apart(name, o, size, **{i: v for i, v in others.items() if v[0] != o})
+                _apart("k_seen" if o == ks else "v_seen", o, size, **{i: v for i, v in others.items() if v[0] != o})
     rc = (_lib or load()).specrouter_kv4_append(
-        x, xs, y, ys, gamma.data_ptr(), kc, kp, vc, vp, _ptr(cache_mask),
-        kv_len.data_ptr(), _ptr(shared_len), ks, vs, B, rows - 1, Hkv, D, L_cap, _ptr(status),
+        x, xs, y, ys, gamma.data_ptr(), kc, kp, vc, vp, None if cache_mask is None else cache_mask.data_ptr(),
+        kv_len.data_ptr(), None if shared_len is None else shared_len.data_ptr(), ks, vs, B, rows - 1, Hkv, D, L_cap, _ptr(status),
         torch._C._cuda_getCurrentRawStream(here))
     if rc:
         _check(rc, "specrouter_kv4_append")
