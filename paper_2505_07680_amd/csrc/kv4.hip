@@ -123,7 +123,7 @@ __device__ __forceinline__ void append_rows(const Append4& a, int b, int cur, in
   }
 }
 
-// A step's few rows: one workgroup per sequence, which reads the cursor once and
+// Few rows: one workgroup per sequence, which reads the cursor once and
 // then is the only writer of the length.
 constexpr int kStepThreads = 1024;
 template <int D>
@@ -145,7 +145,7 @@ kv4_append_step_kernel(Append4 a) {
   if (threadIdx.x == 0) a.kv_len[b] = s.cur + s.n;
 }
 
-// Prompts: workgroups over blocks of rows; the lengths and the mask follow in a
+// More: workgroups over blocks of rows; the lengths and the mask follow in a
 // kernel of their own, when every row's workgroup has read the cursor.
 constexpr int kPromptThreads = 256;
 constexpr int kPromptUnroll = 4;
@@ -187,8 +187,24 @@ auto prompt_kernel(int D) {
 
 }  // namespace
 
-// Rows of a sequence up to which one workgroup appends them.
-constexpr int kStepRows = 1024;
+// Whether one workgroup appends a sequence's rows (all heads counted): up to three of
+// its passes, where one launch less is worth more than more CUs, and up to eight where
+// such workgroups fill more than half of the CUs in one turn. us with one workgroup
+// and with blocks of rows, heads of 128, 64 rows a pass, inputs from HBM:
+//   sequences   3 passes    4           6           8           16
+//        16     7.5  7.6    8.6  7.8   11.2  7.9   13.7  8.1   29.0 10.3
+//        64     8.9  9.3   11.8 10.0   16.4 12.5   20.3 14.0   36.7 20.0
+//       128    11.6 13.2   13.8 14.1   19.1 15.5   22.8 20.5   42.4 33.7
+//       160    12.2 14.3   15.0 15.1   20.3 19.8   25.3 25.1   45.9 40.6
+//       224    14.4 16.0   17.7 20.1   24.4 25.7   30.7 34.2   56.6 53.6
+//       256    15.3 16.1   18.8 20.2   26.4 26.6   33.7 34.4   65.2 59.9
+//       320    22.2 20.7   26.8 23.8   38.6 34.3   48.9 41.2   96.7 72.9
+// One sequence: 6.6 and 6.6 with 3, 21.5 and 6.7 with 16. Heads of 64, 128 rows a pass: the same
+// within 10%.
+bool one_workgroup_each(int B, long rows, int D, int cus) {
+  const long passes = (rows * D + kStepThreads * 8 - 1) / (kStepThreads * 8);
+  return passes <= 3 || (passes <= 8 && B > cus / 2 && B <= cus);
+}
 
 int launch_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* gamma,
                       void* k_codes, void* k_powers, void* v_codes, void* v_powers, uint8_t* cache_mask,
@@ -198,7 +214,9 @@ int launch_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, in
                   (uint8_t*)k_codes, (uint8_t*)k_powers, (uint8_t*)v_codes, (uint8_t*)v_powers, cache_mask, kv_len,
                   shared_len, (uint16_t*)k_seen, (uint16_t*)v_seen, gamma_max, Hkv, L_cap, status};
   const long rows = (long)(gamma_max + 1) * Hkv;
-  if (rows <= kStepRows) {
+  const int cus = device_cu_count();
+  if (cus <= 0) return SR_ELAUNCH;
+  if (one_workgroup_each(B, rows, D, cus)) {
     hipLaunchKernelGGL(D == 64 ? kv4_append_step_kernel<64> : kv4_append_step_kernel<128>, dim3(B), dim3(kStepThreads),
                        0, stream, a);
     return hipGetLastError() == hipSuccess ? SR_OK : SR_ELAUNCH;
