@@ -117,7 +117,12 @@ int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_rows,
   // and stream long. (64 query heads on 8 of 128, us in eight waves and in chunks: one sequence
   // of 1024 positions, 64 rows, 20.0 and 13.6; 16 of 1024 28.8 and 23.4, of 3000
   // 45.5 and 53.7; 32 of 512 25.2 and 24.3, of 640 26.6 and 29.9; 40 of 2048,
-  // 72 rows, 118 and 98, 136 rows 164 and 120; 256 of 512, 72 rows, 217 and 176.)
+  // 72 rows, 118 and 98, 136 rows 164 and 120; 256 of 512, 72 rows, 217 and 176.
+  // Where the jobs divide the CUs, by the keys of a CU, jobs L_cap / 256, over 1 to 32 sequences,
+  // both dimensions, 56 to 192 rows: 256 keys 29 and 23, 512 33 and 31, 750 37 and 38, 1024
+  // 47 and 49, 2048 70 and 82 for 96 rows of 128, at 64 about the same from 400 on. Rows that
+  // chunks save blocks of, 112 of 128 in three, are faster at every length, 136 and 144 up to
+  // 2048 and within 8% beyond; of 64 those lose up to a fifth from 1024 on.)
   bool chunked = false;
   if (window > 0 && plan->qg > 1) {
     const int chunks = (R + 16 * kMaxNQ - 1) / (16 * kMaxNQ);
@@ -218,12 +223,17 @@ int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_rows,
   plan->part_offset = counters;
   size_t bytes = plan->n_splits > 1 ? counters + (size_t)B * Hkv * plan->n_splits * R * (D + 2) * sizeof(float) : 0;
   const long n_jobs = (long)plan->n_splits * pairs;
-  // (With a window, sequences differ by its length at most. Up to 128 keys the order
-  // kernel's 5 us are more than that: 251 sequences of 22 positions 15.1 us with it, 11.6
-  // without; so they are for a few chunks more than fit at once: 33 sequences of 512
-  // positions, 72 rows, 42 and 36.)
+  // With a window, sequences differ by its length at most, and for short ones that is less
+  // than the order kernel's 5 us and the table's reads. With one or two query chunks it is
+  // up to 704 keys, whatever the number of jobs (33 to 256 sequences of half to three
+  // windows, or of up to one; us without and with the order: 32/32 heads of 64, 33 sequences
+  // of 256 positions 16.1 and 20.6, 256 of 704 259 and 254; 64/8 of 128, gamma 8, 128 of
+  // 512 85 and 92, 256 of 704 207 and 205, and of 2 to 512 97 and 123). From three chunks on
+  // the order also brings a pair's chunks together, which then share its keys in an
+  // L2 (64/8 of 128, gamma 16, 256 sequences of 256 150 and 137, of 704 299 and 220), so it
+  // goes only up to 128 keys, or for a few chunks more than fit at once (24 of 512 27 and 31).
   const bool alike = window > 0 && (L_cap <= 2 * kTileKeys ||
-                                    (plan->q_chunks > 1 && L_cap <= 704 && 2 * n_jobs <= 3 * target));
+                                    (L_cap <= 704 && (plan->q_chunks <= 2 || 2 * n_jobs <= 3 * target)));
   plan->ordered = n_jobs > target && !alike ? 1 : 0;
   plan->order_offset = (bytes + 15) / 16 * 16;
   if (plan->ordered) bytes = plan->order_offset + (size_t)n_jobs * sizeof(int32_t);
