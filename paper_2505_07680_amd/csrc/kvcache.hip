@@ -39,7 +39,7 @@ kv_append_kernel(const u32x4* __restrict__ k_new, const u32x4* __restrict__ v_ne
     int n = g + 1;
     uint32_t bad = 0;
     if (g < 0 || g > gmax) bad |= SR_ST_GAMMA;
-    else if (L < 0 || L > L_cap || cur < 0 || cur + n > L_cap) bad |= SR_ST_KVLEN;
+    else if (L < 0 || L > L_cap || cur < 0 || cur > L_cap - n) bad |= SR_ST_KVLEN;
     if (bad) {
       n = 0;
       if (status) atomicOr(status, (int32_t)bad);
