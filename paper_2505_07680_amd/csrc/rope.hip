@@ -16,8 +16,8 @@
 //
 // Bound by HBM for prompts: 4 of 8100 rows, 72 heads of 128, 190 us, 6.3 TB/s read
 // and written (a large device copy reaches 4.9). 256 sequences' steps (30 MB)
-// take 9.7 us, 3.1 TB/s: the launch, the cold caches and one wave's chain of
-// position, loads, angles and store. One token takes 2.4 us, the launch.
+// take 9.8 us, 3.0 TB/s: the launch, the cold caches and one wave's chain of
+// position, loads, angles and store. One token takes 2.5 us, the launch.
 
 #include "caching.h"
 
