@@ -408,10 +408,9 @@ int specrouter_kv_compact(void* k_cache, void* v_cache, uint8_t* cache_mask, int
  * q_out, k_out bf16 [B][gamma_max+1][Hq or Hkv][D] contiguous (what
  *              specrouter_verify_attention and specrouter_kv_append take); may
  *              be q / k themselves where those are contiguous, else they must
- *              not overlap them or each other. (Where q and k start at one
- *              address, queries and keys of the same rows, one of the two may be
- *              in place.) Equal addresses are checked here, ranges by the Python
- *              binding; so in specrouter_kv4_append
+ *              not overlap them or each other (equal addresses are refused here,
+ *              ranges by the Python binding). Where q and k start at one address,
+ *              queries and keys of the same rows, one of the two may be in place
  * Rows i > gamma_b, and all rows of a sequence with bad data, are neither read
  * nor written. Computed in fp32 and rounded to bf16 once; a head of any finite
  * magnitude has its norm (squares outside fp32's range are scaled first).

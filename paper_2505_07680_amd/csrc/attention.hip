@@ -207,16 +207,17 @@ int attention_plan(int B, int gamma_max, int Hq, int Hkv, int D, int cache_rows,
   // them (64 to 8192 normal keys: 1.05e-3 off the 64-bit result with one tile
   // per wave, 1.5e-3 with three), so there the reference follows the tiles
   // (one such key per tile whatever the length: 1.05e-3 again). With a window that costs
-  // a call 3 to 10% (one sequence of 8192 positions, 72 rows, 25.4 and 26.6 us).
-  plan->follow = few ? 1 : 0;
+  // a call 3 to 10% (one sequence of 8192 positions, 72 rows, 25.4 and 26.6 us), so there a
+  // wave of one tile, whose reference is that tile's maximum either way, stays lazy.
+  plan->follow = few && (window == 0 || plan->split_keys > kTileKeys) ? 1 : 0;
   // Rows in chunks with a window are as exact as the two groups without one: where those
   // follow, or leave a wave one tile, a wave of several tiles follows here. (2 sequences
   // of 2048 keys, 72 rows: 1.52e-3 off where the reference is lazy, 1.01e-3 where it follows.)
-  if (chunked) {
+  if (chunked && plan->split_keys > kTileKeys) {
     AttentionPlan groups;
-    const int rc = plan->split_keys > kTileKeys ? attention_plan(B, gamma_max, Hq, Hkv, D, L_cap, 0, 0, &groups) : SR_OK;
+    const int rc = attention_plan(B, gamma_max, Hq, Hkv, D, L_cap, 0, 0, &groups);
     if (rc != SR_OK) return rc;
-    plan->follow = plan->split_keys > kTileKeys && (groups.follow || groups.split_keys <= kTileKeys) ? 1 : 0;
+    plan->follow = groups.follow || groups.split_keys <= kTileKeys ? 1 : 0;
   }
   // [arrival counters: B*Hkv*q_chunks, one per 128-byte line][partial o][partial (m, l)][order]
   const size_t counters = (size_t)B * Hkv * plan->q_chunks * kCounterStride * sizeof(uint32_t);
